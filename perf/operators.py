@@ -84,8 +84,8 @@ def draw(rng):
             c["state"] = c["F"] != 1 and rng.random() < 0.4          # (one tap has no rows before the first)
             c["ragged"] = N > 1 and rng.random() < 0.5
         cost = N * L * C * max(1, c["S"]) * (2 if op == "scan_grad" else 1)
-        # no dearer than the largest listed cases; a loop over tokens that the plain form takes in seconds
-        if cost > 4 * 2048 * 4096 * 16 * (2 if op.startswith("scan") else 0.125):
+        # no dearer than the largest listed cases, in arithmetic and in memory
+        if cost > 4 * 2048 * 4096 * 16 * (2 if op.startswith("scan") else 0.125) or work(c)["bytes"] > 5.4e8:
             continue
         del c["name"]
         return c
