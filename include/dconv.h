@@ -70,8 +70,9 @@ typedef enum dconv_status {
                                  does not fit the kernels' 32-bit indexing       */
     DCONV_UNSUPPORTED = 3,    /* the requested variant cannot run this shape     */
     DCONV_LAUNCH_FAILED = 4,  /* the HIP runtime reported an error at launch     */
-    DCONV_SCRATCH_EXCEEDED = 5/* dconv_general_noalloc only: the launch would need
-                                 more scratch memory than the static array holds */
+    DCONV_SCRATCH_EXCEEDED = 5/* dconv_general_noalloc: the launch would need more
+                                 scratch memory than the static array holds; sequence
+                                 operators: the caller's workspace is too small    */
 } dconv_status;
 
 /* Kernel variants accepted by the *_v entry points. */
@@ -214,7 +215,8 @@ int dconv_general_v(const float *in, int N, int C, int H, int W,
  * Errors as for dconv_general; a base pointer that is not 2-byte aligned ->
  * DCONV_BAD_SHAPE.
  */
-enum { DCONV_DTYPE_F16 = 0, DCONV_DTYPE_BF16 = 1, DCONV_DTYPE_I8 = 2 };
+enum { DCONV_DTYPE_F16 = 0, DCONV_DTYPE_BF16 = 1, DCONV_DTYPE_I8 = 2,
+       DCONV_DTYPE_F32 = 3 /* the sequence operators below only */ };
 int dconv_general_f16(const void *in, int N, int C, int H, int W,
                       const void *filt, int K, int F,
                       float *out, void *stream);
@@ -387,6 +389,129 @@ int dconv_release_workspace(void);
 int dconv_general_noalloc(const float *in, int N, int C, int H, int W,
                           const float *filt, int K, int F,
                           float *out, int variant, void *stream);
+
+/*
+ * Convolutions over the tokens of sequences.  Two operators follow each other in
+ * a state space layer: a short CAUSAL convolution, one filter of F taps for each
+ * channel, and a SCAN, the recurrence whose kernel the inputs choose token by
+ * token.  Each has three forms: whole prompts, their gradients, and one token at
+ * a time on a cache of states.  Letters: N sequences, L tokens, C channels, F
+ * taps, S states a channel, G groups.
+ *
+ * Rules beside the common ones at the top
+ *   - Element types: DCONV_DTYPE_F16, _BF16 or _F32, one for all token tensors,
+ *     filters and biases of a call; what is declared `float` is fp32 whatever the
+ *     type.  Arithmetic, sums and states are fp32, every output is rounded once.
+ *   - Token tensors are [N][L][C] with the channels next to each other and any
+ *     strides between tokens and sequences, so slices of a wider projection need
+ *     no copy; data need only be aligned to its element.  The tokens of an output
+ *     must not overlap.
+ *   - lengths [N] (int32, device; NULL: all L) are the tokens of each sequence in
+ *     a padded batch, 0 to L; values outside are taken as the nearest of these.
+ *     What lies behind is not used, whatever it holds, and the outputs there
+ *     (gradients too) are written as 0.
+ *   - slots [N] (int32, device; NULL: row n has slot n, and M >= N) of the step
+ *     forms say which of the M rows of a cache belongs to each row of the call.  A
+ *     row whose slot is not in 0..M-1, or is that of an earlier row, is padding: its
+ *     outputs are written as 0 and no state is touched.
+ *   - The state that a prompt leaves may be written over the one that it read
+ *     (state_out == state); apart from that outputs must not overlap inputs.
+ *   - Nothing is allocated, no call synchronises, results are the same bits on
+ *     every call, and all calls may be captured.  What a call needs between its
+ *     kernels lies in the caller's workspace (16-byte aligned; sizes from
+ *     dconv_causal_workspace and dconv_scan_workspace), which is free again when the
+ *     call's work on the stream is done: calls that may run at the same time,
+ *     graphs among them, need one each.
+ *   - Errors: a required pointer (or the argument struct) that is NULL ->
+ *     DCONV_NULL_POINTER; a size <= 0, F > 8, S > 32, C not a multiple of G, more
+ *     than 2^30 tokens of a sequence, work beyond 2^31-1 workgroups, misaligned
+ *     data -> DCONV_BAD_SHAPE; another element type -> DCONV_UNSUPPORTED; a workspace that
+ *     is too small -> DCONV_SCRATCH_EXCEEDED.
+ */
+typedef struct dconv_tokens {
+    void *p;               /* sequence 0, token 0                                   */
+    long long sn, sl, sg;  /* elements from a sequence, a token, a group to the next
+                              (sg: only where there are groups)                     */
+} dconv_tokens;
+
+/*
+ * dconv_causal:  s[n][t][c] = bias[c] + sum_j filt[c][j] * x[n][t - (F-1) + j][c]
+ *                out = s * sigmoid(s) with silu, s without
+ * Rows before token 0 come from state [N][F-1][C] (NULL: zeros), the F-1 rows
+ * before the sequence's end go to state_out, laid out alike (NULL: not wanted).
+ * dconv_causal_grad: from dout = d/d out the gradients of x, filt, bias (fp32) and
+ * state; dstate_out is the gradient of state_out (NULL: none).  dfilt, dbias and
+ * dstate may be NULL, dx may not.  Needs a workspace.
+ * dconv_causal_step: L = 1; state_out [M][F-1][C] is a cache of windows, of which
+ * row slots[n] is read and moved on by one token.  `state` is not used.
+ */
+typedef struct dconv_causal_args {
+    int dtype, N, L, C, F, M, silu, reserved;
+    dconv_tokens x, out, dout, dx;
+    const void *filt;            /* [C][F]                                  */
+    const void *bias;            /* [C], may be NULL                        */
+    const void *state;
+    void *state_out;
+    const void *dstate_out;
+    void *dstate;
+    float *dfilt, *dbias;        /* [C][F], [C]                             */
+    const int *lengths, *slots;
+    void *workspace;
+    long long workspace_bytes;
+} dconv_causal_args;
+int dconv_causal(const dconv_causal_args *a, void *stream);
+int dconv_causal_grad(const dconv_causal_args *a, void *stream);
+int dconv_causal_step(const dconv_causal_args *a, void *stream);
+/* Bytes that dconv_causal_grad needs for these sizes (only sizes and dtype are
+ * looked at), -1 where they are not valid; host arithmetic.  The other two forms
+ * need none. */
+long long dconv_causal_workspace(const dconv_causal_args *a);
+
+/*
+ * dconv_scan, for every channel c of group g = c / (C / G):
+ *   d[t] = softplus(delta[t] + delta_bias)    (delta + delta_bias without softplus)
+ *   h[t][s] = exp(d[t] * A[c][s]) * h[t-1][s] + d[t] * u[t] * B[t][g][s]
+ *   y[t] = sum_s C[t][g][s] * h[t][s] + D[c] * u[t]
+ *   out = y * z * sigmoid(z) with a gate z, y without
+ * h before token 0 is state [N][C][S] (NULL: zeros), h behind the sequence's end
+ * goes to state_out (NULL: not wanted).  `starts` (NULL: not wanted) keeps states
+ * on the way, dconv_scan_starts bytes of the library's own layout, from which
+ * dconv_scan_grad goes back; with out.p NULL only starts and state_out are made
+ * (Cm, D and z are not read then).
+ * dconv_scan_grad: from dout the gradients of all inputs; dstate_out is the
+ * gradient of state_out (NULL: none).  Required are du, ddelta, dB, dC and dA, and
+ * dz where there is a gate; dD, ddelta_bias and dstate may be NULL.  starts are
+ * those that dconv_scan left for the same inputs, or NULL: they are made again.
+ * dconv_scan_step: L = 1; state_out [M][C][S] is a cache of states, of which row
+ * slots[n] is read and updated.  `state` is not used.
+ * Decays exp(d * A) are meant to be at most 1 (A <= 0, d >= 0); larger ones are
+ * computed as they are, and overflow where the recurrence does.
+ */
+typedef struct dconv_scan_args {
+    int dtype, N, L, C, S, G, M, softplus;
+    dconv_tokens u, delta, z, out;         /* z.p may be NULL                  */
+    dconv_tokens B, Cm;                    /* [N][L][G][S], the S together     */
+    dconv_tokens dout, du, ddelta, dz, dB, dC;
+    const float *A;                        /* [C][S]                           */
+    const float *D, *delta_bias;           /* [C], may be NULL                 */
+    const float *state;
+    float *state_out;
+    const float *dstate_out;
+    float *dstate;
+    float *dA, *dD, *ddelta_bias;          /* [C][S], [C], [C]                 */
+    void *starts;
+    const int *lengths, *slots;
+    void *workspace;
+    long long workspace_bytes;
+} dconv_scan_args;
+int dconv_scan(const dconv_scan_args *a, void *stream);
+int dconv_scan_grad(const dconv_scan_args *a, void *stream);
+int dconv_scan_step(const dconv_scan_args *a, void *stream);
+/* Bytes of workspace for dconv_scan (grad == 0; 0 bytes for some) or dconv_scan_grad
+ * (looks at the sizes, dtype and whether starts is NULL), and of `starts`; -1 where
+ * the sizes are not valid.  Host arithmetic. */
+long long dconv_scan_workspace(const dconv_scan_args *a, int grad);
+long long dconv_scan_starts(const dconv_scan_args *a);
 
 /* Human-readable name of a status code; static storage, never NULL. */
 const char *dconv_status_string(int status);

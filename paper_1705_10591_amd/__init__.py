@@ -1,4 +1,7 @@
-"""MI355X-native direct fp32 2D convolution (gfx950): Python binding of libdconv.so.
+"""MI355X-native direct convolution (gfx950): Python binding of libdconv.so.
+
+2D convolutions of images are here, the causal convolution and the scan over tokens of sequences in `sequence`,
+whose functions are this package's too.
 
 The functions here only marshal arguments: they take torch CUDA tensors
 (device memory and the current stream come from PyTorch), pass raw device
@@ -13,6 +16,10 @@ import ctypes
 from pathlib import Path
 
 import torch
+
+from . import sequence as _sequence
+from .sequence import (CausalGrad, ScanGrad, dconv_causal, dconv_causal_grad, dconv_causal_step, dconv_scan,  # noqa: F401
+                       dconv_scan_grad, dconv_scan_step, scan_starts)
 
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libdconv.so"
@@ -29,8 +36,8 @@ EXPORTS = ("dconv_single_channel", "dconv_general", "dconv_single_channel_v",
            "dconv_general_v", "dconv_status_string", "dconv_version",
            "dconv_tile_config_count", "dconv_tile_choice", "dconv_kernel_choice", "dconv_release_workspace",
            "dconv_general_f16", "dconv_general_bf16", "dconv_general_half_v",
-           "dconv_general_i8", "dconv_general_i8_v", "dconv_general_lowp", "dconv_general_noalloc")
-DTYPE_F16, DTYPE_BF16, DTYPE_I8 = 0, 1, 2
+           "dconv_general_i8", "dconv_general_i8_v", "dconv_general_lowp", "dconv_general_noalloc") + _sequence.EXPORTS
+DTYPE_F16, DTYPE_BF16, DTYPE_I8, DTYPE_F32 = 0, 1, 2, _sequence.DTYPE_F32
 LAYOUT_CHANNELS_LAST, LAYOUT_CHANNEL_BLOCKED = 0, 1
 
 _lib = None
@@ -75,6 +82,7 @@ def load_library() -> ctypes.CDLL:
         lib.dconv_tile_choice.restype = i
         lib.dconv_kernel_choice.argtypes = [i] * 7
         lib.dconv_kernel_choice.restype = i
+        _sequence.declare(lib)
         lib.dconv_status_string.argtypes = [i]
         lib.dconv_status_string.restype = ctypes.c_char_p
         _lib = lib

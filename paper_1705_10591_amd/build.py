@@ -25,7 +25,8 @@ SOURCES = [("api.hip", [], "api"), ("simple.hip", [], "simple"), ("single.hip", 
           [("few_taps_inst.hip", [f"-DDCONV_F={f}"], f"few_taps_f{f}") for f in range(1, 8)] + \
           [("split_taps.hip", [], "split_taps"), ("short.hip", [], "short")] + \
           [("half.hip", [], "half"), ("half_1x1.hip", [], "half_1x1"), ("half_short.hip", [], "half_short")] + \
-          [("half_inst.hip", [f"-DDCONV_F={f}"], f"half_f{f}") for f in range(1, 33)]
+          [("half_inst.hip", [f"-DDCONV_F={f}"], f"half_f{f}") for f in range(1, 33)] + \
+          [("causal.hip", [], "causal"), ("scan.hip", [], "scan"), ("scan_grad.hip", [], "scan_grad"), ("scan_step.hip", [], "scan_step")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms are switched off for all device code (the host pass

@@ -279,7 +279,7 @@ const char* dconv_status_string(int status)
     case DCONV_BAD_SHAPE: return "bad shape";
     case DCONV_UNSUPPORTED: return "variant does not support this shape";
     case DCONV_LAUNCH_FAILED: return "kernel launch failed";
-    case DCONV_SCRATCH_EXCEEDED: return "shape needs more scratch memory than the static device array holds";
+    case DCONV_SCRATCH_EXCEEDED: return "call needs more scratch memory than the static device array or its workspace holds";
     default: return "unknown status";
     }
 }
@@ -340,6 +340,6 @@ int dconv_release_workspace(void)
     return DCONV_OK;
 }
 
-int dconv_version(void) { return 1015; }
+int dconv_version(void) { return 1016; }
 
 }  // extern "C"

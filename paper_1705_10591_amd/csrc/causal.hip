@@ -1,0 +1,446 @@
+// The causal convolution over tokens: one filter of F taps for every channel, s[t] = bias + sum_j filt[j] x[t-(F-1)+j],
+// out = s sigmoid(s) or s.
+//
+// With F multiply-adds an element the call is bound by memory: x is read once and out is written once.  The paper's
+// sliding window (Sec. 3: a thread keeps the rows that its next output needs in registers and reads one new row a
+// step) does that along the tokens: a thread has a run of V channels (16 bytes) and walks a strip of tokens with the
+// last F-1 rows in registers, kAhead rows in flight; lanes next to each other have runs next to each other.  Only the
+// F-1 rows before a strip are read twice.
+#include "tokens.h"
+
+namespace dconv {
+
+namespace {
+
+constexpr int kAhead = 8;            // rows of a strip that are read together; strips are multiples of it, so that
+                                     // only the first one reaches into the state (F - 1 <= 7 rows)
+
+struct CausalParams {
+    const void *x, *filt, *bias, *state, *dout, *dstate_out;
+    void *out, *state_out, *dx, *dstate;
+    float* part;
+    const int *lengths, *slots;
+    int64_t x_n, x_l, o_n, o_l, g_n, g_l, d_n, d_l;
+    int L, C, M, silu;
+    int vb, sb, vgroups, sgroups, strip;   // runs and strips of a workgroup, groups of each, tokens of a strip
+    int64_t total;
+};
+
+// Where a thread works: sequence n, its first channel c and how many of the V exist, its first token.
+struct Place { int n, c, nv, t0, run, strip; int64_t row; bool ok; };
+
+template <int V> __device__ __forceinline__ Place place_of(const CausalParams& p)
+{
+    const int64_t b = near_block(blockIdx.x, p.total);
+    const int vg = (int)(b % p.vgroups);
+    Place a;
+    a.row = b / p.vgroups;
+    const int sg = (int)(a.row % p.sgroups);
+    a.n = (int)(a.row / p.sgroups);
+    a.strip = threadIdx.x / p.vb;
+    a.run = threadIdx.x - a.strip * p.vb;
+    a.c = (vg * p.vb + a.run) * V;
+    a.nv = min(V, p.C - a.c);
+    const int64_t t0 = ((int64_t)sg * p.sb + a.strip) * p.strip;
+    a.t0 = (int)min(t0, (int64_t)p.L);
+    a.ok = a.strip < p.sb && a.nv > 0 && t0 < p.L;
+    return a;
+}
+
+template <typename T, int F, int V>
+__device__ __forceinline__ void load_filter(const T* filt, int c, int nv, float (&w)[F][V])
+{
+    float flat[F * V];
+#pragma unroll
+    for (int q = 0; q < F; ++q) {
+        float part[V];
+        load_some<V>(filt + (int64_t)c * F + q * V, nv * F - q * V, part);
+#pragma unroll
+        for (int i = 0; i < V; ++i) flat[q * V + i] = part[i];
+    }
+#pragma unroll
+    for (int j = 0; j < F; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[j][i] = flat[i * F + j];
+}
+
+template <typename T, int F, int V>
+__global__ void __launch_bounds__(kThreads)
+causal_kernel(CausalParams p)
+{
+    const Place a = place_of<V>(p);
+    if (!a.ok) return;
+    const int len = length_of(p.lengths, a.n, p.L), end = min(a.t0 + p.strip, p.L);
+    const T* x = (const T*)p.x + a.n * p.x_n + a.c;
+    T* out = (T*)p.out + a.n * p.o_n + a.c;
+    const int64_t first = (int64_t)a.n * (F - 1) * p.C + a.c;
+
+    float w[F][V], bias[V] = {}, rows[kAhead + F - 1][V];
+    load_filter<T, F, V>((const T*)p.filt, a.c, a.nv, w);
+    if (p.bias) load_some<V>((const T*)p.bias + a.c, a.nv, bias);
+#pragma unroll
+    for (int r = 0; r < F - 1; ++r) {
+        const int t = a.t0 - (F - 1) + r;
+        if (t >= 0) {
+            if (t < len) load_some<V>(x + t * p.x_l, a.nv, rows[r]);
+        } else if (p.state) {
+            load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv, rows[r]);
+        } else {
+            for (int i = 0; i < V; ++i) rows[r][i] = 0.f;
+        }
+    }
+    // the last F-1 rows of the sequence, by the thread that has read the state's (which they may overwrite)
+    if (a.t0 == 0 && p.state_out) {
+        for (int r = 0; r < F - 1; ++r) {
+            const int t = len - (F - 1) + r;
+            float v[V] = {};
+            if (t >= 0) load_some<V>(x + t * p.x_l, a.nv, v);
+            else if (p.state) load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv, v);
+            store_some<V>((T*)p.state_out + first + (int64_t)r * p.C, a.nv, v);
+        }
+    }
+    for (int t0 = a.t0; t0 < end; t0 += kAhead) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (t0 + k < min(end, len)) load_some<V>(x + (t0 + k) * p.x_l, a.nv, rows[F - 1 + k]);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            float y[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float s = bias[i];
+#pragma unroll
+                for (int j = 0; j < F; ++j) s = __builtin_fmaf(w[j][i], rows[k + j][i], s);
+                y[i] = t0 + k < len ? (p.silu ? s * sigmoid(s) : s) : 0.f;
+            }
+            if (t0 + k < end) store_some<V>(out + (t0 + k) * p.o_l, a.nv, y);
+        }
+#pragma unroll
+        for (int r = 0; r < F - 1; ++r)
+#pragma unroll
+            for (int i = 0; i < V; ++i) rows[r][i] = rows[kAhead + r][i];
+    }
+}
+
+// Gradients.  With ds[t] = dout[t] silu'(s[t]) (s computed again): dx[r] = sum_j filt[j] ds[r + F-1-j], so a row of dx is
+// done F-1 tokens later and a strip walks F-1 tokens beyond its end; dfilt[j] = sum_t ds[t] x[t-(F-1)+j] and
+// dbias = sum_t ds[t] are summed over the strip by each thread, over the strips of a workgroup in LDS, and by
+// causal_sum_kernel over workgroups, always in the same order.  Bound by memory like the convolution: x and dout
+// in, dx out.
+template <typename T, int F, int V>
+__global__ void __launch_bounds__(kThreads)
+causal_grad_kernel(CausalParams p)
+{
+    __shared__ float red[kThreads * V];
+    const Place a = place_of<V>(p);
+    float acc[F + 1][V] = {};
+    if (a.ok) {
+        const int len = length_of(p.lengths, a.n, p.L), end = min(a.t0 + p.strip, p.L);
+        const T* x = (const T*)p.x + a.n * p.x_n + a.c;
+        const T* dout = (const T*)p.dout + a.n * p.g_n + a.c;
+        T* dx = (T*)p.dx + a.n * p.d_n + a.c;
+        const int64_t first = (int64_t)a.n * (F - 1) * p.C + a.c;
+        float w[F][V], bias[V] = {}, rows[F][V], ds[F][V] = {};
+        load_filter<T, F, V>((const T*)p.filt, a.c, a.nv, w);
+        if (p.bias) load_some<V>((const T*)p.bias + a.c, a.nv, bias);
+#pragma unroll
+        for (int r = 0; r < F - 1; ++r) {            // rows[1 ..]: they move down by one before each token
+            const int t = a.t0 - (F - 1) + r;
+            for (int i = 0; i < V; ++i) rows[r + 1][i] = 0.f;
+            if (t >= 0) {
+                if (t < len) load_some<V>(x + t * p.x_l, a.nv, rows[r + 1]);
+            } else if (p.state) {
+                load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv, rows[r + 1]);
+            }
+        }
+        const int64_t stop = (int64_t)end + F - 1;
+        for (int64_t t0 = a.t0; t0 < stop; t0 += 4) {
+            float xn[4][V], gn[4][V];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                for (int i = 0; i < V; ++i) xn[k][i] = gn[k][i] = 0.f;
+                if (t0 + k < min(stop, (int64_t)len)) {
+                    load_some<V>(x + (t0 + k) * p.x_l, a.nv, xn[k]);
+                    load_some<V>(dout + (t0 + k) * p.g_l, a.nv, gn[k]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t t = t0 + k;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+#pragma unroll
+                    for (int j = 0; j < F - 1; ++j) { rows[j][i] = rows[j + 1][i]; ds[j][i] = ds[j + 1][i]; }
+                    rows[F - 1][i] = xn[k][i];
+                    float s = bias[i], d = gn[k][i];
+#pragma unroll
+                    for (int j = 0; j < F; ++j) s = __builtin_fmaf(w[j][i], rows[j][i], s);
+                    if (p.silu) {
+                        const float sg = sigmoid(s);
+                        d *= sg * (1.f + s * (1.f - sg));
+                    }
+                    d = t < len ? d : 0.f;
+                    ds[F - 1][i] = d;
+                    if (t < end) {
+#pragma unroll
+                        for (int j = 0; j < F; ++j) acc[j][i] = __builtin_fmaf(d, rows[j][i], acc[j][i]);
+                        acc[F][i] += d;
+                    }
+                }
+                // the row that has all of its terms now; before token 0 it is one of the state
+                const int64_t r = t - (F - 1);
+                if (r < end && (r >= a.t0 || (a.t0 == 0 && p.dstate))) {
+                    float v[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        v[i] = 0.f;
+#pragma unroll
+                        for (int j = 0; j < F; ++j) v[i] = __builtin_fmaf(w[j][i], ds[F - 1 - j][i], v[i]);
+                    }
+                    const int64_t i = r - len + F - 1;           // of state_out, if it went there
+                    if (p.dstate_out && i >= 0 && i < F - 1) {
+                        float e[V];
+                        load_some<V>((const T*)p.dstate_out + first + i * p.C, a.nv, e);
+                        for (int k2 = 0; k2 < V; ++k2) v[k2] += e[k2];
+                    }
+                    if (r >= 0) store_some<V>(dx + r * p.d_l, a.nv, v);
+                    else store_some<V>((T*)p.dstate + first + (F - 1 + r) * p.C, a.nv, v);
+                }
+            }
+        }
+    }
+    if (!p.part) return;
+#pragma unroll
+    for (int q = 0; q <= F; ++q) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[threadIdx.x * V + i] = acc[q][i];
+        __syncthreads();
+        if (a.strip == 0 && a.nv > 0) {
+            float* to = p.part + (a.row * (F + 1) + q) * p.C + a.c;
+            for (int i = 0; i < V; ++i) {
+                float s = 0.f;
+                for (int k = 0; k < p.sb; ++k) s += red[(k * p.vb + a.run) * V + i];
+                if (i < a.nv) to[i] = s;
+            }
+        }
+    }
+}
+
+// dfilt[c][j] and dbias[c] from `rows` parts [F + 1][C]: four waves take a quarter of the rows each.
+__global__ void __launch_bounds__(kThreads)
+causal_sum_kernel(const float* part, int64_t rows, int C, int F, float* dfilt, float* dbias)
+{
+    __shared__ float red[kThreads];
+    const int64_t col = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave, cols = (int64_t)(F + 1) * C;
+    const int w = threadIdx.x / kWave;
+    float s = 0.f;
+    if (col < cols)
+        for (int64_t r = w; r < rows; r += 4) s += part[r * cols + col];
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (w || col >= cols) return;
+    s = (red[threadIdx.x] + red[threadIdx.x + 64]) + (red[threadIdx.x + 128] + red[threadIdx.x + 192]);
+    const int j = (int)(col / C), c = (int)(col % C);
+    if (j < F) {
+        if (dfilt) dfilt[(int64_t)c * F + j] = s;
+    } else if (dbias) {
+        dbias[c] = s;
+    }
+}
+
+// One token of each row: the window of F-1 rows is read, used with the new one and written back moved by one.
+template <typename T, int F, int V>
+__global__ void __launch_bounds__(kThreads)
+causal_step_kernel(CausalParams p)
+{
+    const int n = blockIdx.x / p.vgroups;
+    const int slot = slot_of(p.slots, n, p.M);
+    const int c = ((blockIdx.x - n * p.vgroups) * kThreads + threadIdx.x) * V, nv = min(V, p.C - c);
+    if (nv <= 0) return;
+    T* out = (T*)p.out + n * p.o_n + c;
+    float y[V] = {};
+    if (slot >= 0) {
+        float w[F][V], rows[F][V];
+        T* st = (T*)p.state_out + (int64_t)slot * (F - 1) * p.C + c;
+#pragma unroll
+        for (int r = 0; r < F - 1; ++r) load_some<V>(st + (int64_t)r * p.C, nv, rows[r]);
+        load_some<V>((const T*)p.x + n * p.x_n + c, nv, rows[F - 1]);
+        load_filter<T, F, V>((const T*)p.filt, c, nv, w);
+        if (p.bias) load_some<V>((const T*)p.bias + c, nv, y);
+#pragma unroll
+        for (int r = 0; r < F - 1; ++r) store_some<V>(st + (int64_t)r * p.C, nv, rows[r + 1]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float s = y[i];
+#pragma unroll
+            for (int j = 0; j < F; ++j) s = __builtin_fmaf(w[j][i], rows[j][i], s);
+            y[i] = p.silu ? s * sigmoid(s) : s;
+        }
+    }
+    store_some<V>(out, nv, y);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+constexpr int kMaxTaps = 8;
+constexpr int64_t kMaxBlocks = 2147483647LL;
+
+bool sizes_ok(const dconv_causal_args& a)
+{
+    return a.N > 0 && a.L > 0 && a.L <= kMaxTokens && a.C > 0 && a.F > 0 && a.F <= kMaxTaps &&
+           (double)a.N * a.L * a.C < kMaxElements;
+}
+
+// Elements of a run: 16 bytes, half of that in gradients of more than four taps, whose windows and sums of 8 channels
+// would not fit the registers.
+int run_of(const dconv_causal_args& a, bool grad)
+{
+    const int v = 16 / token_bytes(a.dtype);
+    return grad && a.F > 4 && v == 8 ? 4 : v;
+}
+
+// Runs and strips of a workgroup (at most 256 threads, `most` runs) and the length of a strip: long ones read fewer
+// rows twice, short ones fill the chip.
+void lay_out(const dconv_causal_args& a, bool grad, CausalParams* p)
+{
+    const int V = run_of(a, grad), runs = (a.C - 1) / V + 1, most = grad ? 64 : kThreads;
+    p->vgroups = (runs + most - 1) / most;
+    p->vb = (runs + p->vgroups - 1) / p->vgroups;
+    p->sb = kThreads / p->vb;
+    p->strip = grad ? 64 : 32;
+    while (p->strip > kAhead && (double)a.N * runs * ((a.L + p->strip - 1) / p->strip) < 262144.0) p->strip /= 2;
+    const int64_t strips = ((int64_t)a.L + p->strip - 1) / p->strip;
+    if (strips < p->sb) p->sb = (int)strips;
+    p->sgroups = (int)((strips + p->sb - 1) / p->sb);
+    p->total = (int64_t)a.N * p->sgroups * p->vgroups;
+}
+
+int check(const dconv_causal_args* a, bool step, bool grad)
+{
+    if (!a) return DCONV_NULL_POINTER;
+    const int e = token_bytes(a->dtype);
+    if (!e) return DCONV_UNSUPPORTED;
+    if (!sizes_ok(*a) || (step && (a->L != 1 || a->M <= 0 || (!a->slots && a->M < a->N)))) return DCONV_BAD_SHAPE;
+    if (!a->x.p || !a->filt || (!grad && !a->out.p) || (grad && (!a->dout.p || !a->dx.p))) return DCONV_NULL_POINTER;
+    if (step && a->F > 1 && !a->state_out) return DCONV_NULL_POINTER;
+    for (const void* q : {(const void*)a->x.p, (const void*)a->out.p, (const void*)a->dout.p, (const void*)a->dx.p, a->filt,
+                          a->bias, a->state, (const void*)a->state_out, a->dstate_out, (const void*)a->dstate})
+        if (!aligned_to(q, e)) return DCONV_BAD_SHAPE;
+    for (const void* q : {(const void*)a->dfilt, (const void*)a->dbias, (const void*)a->lengths, (const void*)a->slots})
+        if (!aligned_to(q, 4)) return DCONV_BAD_SHAPE;
+    return DCONV_OK;
+}
+
+CausalParams params_of(const dconv_causal_args& a)
+{
+    CausalParams p{};
+    p.x = a.x.p; p.filt = a.filt; p.bias = a.bias; p.state = a.state; p.dout = a.dout.p; p.dstate_out = a.dstate_out;
+    p.out = a.out.p; p.state_out = a.state_out; p.dx = a.dx.p; p.dstate = a.dstate;
+    p.lengths = a.lengths; p.slots = a.slots;
+    p.x_n = a.x.sn; p.x_l = a.x.sl; p.o_n = a.out.sn; p.o_l = a.out.sl;
+    p.g_n = a.dout.sn; p.g_l = a.dout.sl; p.d_n = a.dx.sn; p.d_l = a.dx.sl;
+    p.L = a.L; p.C = a.C; p.M = a.M; p.silu = a.silu;
+    return p;
+}
+
+enum class Form { kPrompt, kGrad, kStep };
+
+template <typename T, int F> int launch(Form form, const CausalParams& p, hipStream_t st)
+{
+    constexpr int V = 16 / sizeof(T), VG = V == 8 && F > 4 ? 4 : V;
+    if (p.total > kMaxBlocks) return DCONV_BAD_SHAPE;
+    const dim3 grid((unsigned)p.total);
+    begin_launch();
+    switch (form) {
+    case Form::kPrompt: hipLaunchKernelGGL((causal_kernel<T, F, V>), grid, dim3(kThreads), 0, st, p); break;
+    case Form::kGrad: hipLaunchKernelGGL((causal_grad_kernel<T, F, VG>), grid, dim3(kThreads), 0, st, p); break;
+    case Form::kStep: hipLaunchKernelGGL((causal_step_kernel<T, F, V>), grid, dim3(kThreads), 0, st, p); break;
+    }
+    return launch_status();
+}
+
+template <typename T> int launch_taps(Form form, int F, const CausalParams& p, hipStream_t st)
+{
+    switch (F) {
+    case 1: return launch<T, 1>(form, p, st);
+    case 2: return launch<T, 2>(form, p, st);
+    case 3: return launch<T, 3>(form, p, st);
+    case 4: return launch<T, 4>(form, p, st);
+    case 5: return launch<T, 5>(form, p, st);
+    case 6: return launch<T, 6>(form, p, st);
+    case 7: return launch<T, 7>(form, p, st);
+    default: return launch<T, 8>(form, p, st);
+    }
+}
+
+int launch_typed(Form form, const dconv_causal_args& a, const CausalParams& p, hipStream_t st)
+{
+    switch (a.dtype) {
+    case DCONV_DTYPE_F16: return launch_taps<_Float16>(form, a.F, p, st);
+    case DCONV_DTYPE_BF16: return launch_taps<__bf16>(form, a.F, p, st);
+    default: return launch_taps<float>(form, a.F, p, st);
+    }
+}
+
+int64_t part_rows(const CausalParams& p) { return p.total / p.vgroups; }
+
+}  // namespace
+
+}  // namespace dconv
+
+using namespace dconv;
+
+extern "C" {
+
+int dconv_causal(const dconv_causal_args* a, void* stream)
+{
+    const int rc = check(a, false, false);
+    if (rc != DCONV_OK) return rc;
+    CausalParams p = params_of(*a);
+    lay_out(*a, false, &p);
+    return launch_typed(Form::kPrompt, *a, p, (hipStream_t)stream);
+}
+
+long long dconv_causal_workspace(const dconv_causal_args* a)
+{
+    if (!a || !token_bytes(a->dtype) || !sizes_ok(*a)) return -1;
+    CausalParams p{};
+    lay_out(*a, true, &p);
+    return part_rows(p) * (a->F + 1) * a->C * 4;
+}
+
+int dconv_causal_grad(const dconv_causal_args* a, void* stream)
+{
+    int rc = check(a, false, true);
+    if (rc != DCONV_OK) return rc;
+    CausalParams p = params_of(*a);
+    lay_out(*a, true, &p);
+    const bool sums = a->dfilt || a->dbias;
+    if (sums) {
+        if (!a->workspace) return DCONV_NULL_POINTER;
+        if (!aligned_to(a->workspace, 16)) return DCONV_BAD_SHAPE;
+        if (a->workspace_bytes < dconv_causal_workspace(a)) return DCONV_SCRATCH_EXCEEDED;
+        p.part = (float*)a->workspace;
+    }
+    rc = launch_typed(Form::kGrad, *a, p, (hipStream_t)stream);
+    if (rc != DCONV_OK || !sums) return rc;
+    const int64_t cols = (int64_t)(a->F + 1) * a->C;
+    begin_launch();
+    hipLaunchKernelGGL(causal_sum_kernel, dim3((unsigned)((cols + kWave - 1) / kWave)), dim3(kThreads), 0, (hipStream_t)stream,
+                       p.part, part_rows(p), a->C, a->F, a->dfilt, a->dbias);
+    return launch_status();
+}
+
+int dconv_causal_step(const dconv_causal_args* a, void* stream)
+{
+    const int rc = check(a, true, false);
+    if (rc != DCONV_OK) return rc;
+    CausalParams p = params_of(*a);
+    const int per = kThreads * (16 / token_bytes(a->dtype));
+    p.vgroups = (a->C - 1) / per + 1;
+    p.total = (int64_t)a->N * p.vgroups;
+    return launch_typed(Form::kStep, *a, p, (hipStream_t)stream);
+}
+
+}  // extern "C"

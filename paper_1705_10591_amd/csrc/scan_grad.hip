@@ -1,0 +1,394 @@
+// Gradients of the scan over tokens (scan_kernel.h says how the work is divided).
+//
+// With dy = dout z sigmoid(z), a = exp(d A) and g[t] the gradient of h[t]:
+//   g[t]  = C[t] dy[t] + a[t+1] g[t+1]
+//   dC[t] = sum_c dy h[t],  dB[t] = sum_c g d u,  q = sum_s g B,  e = g a h[t-1]
+//   du = d q + D dy,  d(delta) = (sum_s e A + u q) sigmoid(delta + bias),  dA = sum_t e d,  dz = dout y (z sigmoid(z))'
+// States are needed in the order opposite to the one they are made in: they are kept at the start of every tile
+// (`starts`), and a tile of 16 tokens makes its own again in registers, 4 decays and 4 states a token and lane, before it
+// walks back.  About 20 vector instructions for each (token, channel, state) bound the call, not its memory.
+//
+// dB and dC are sums over channels, that is over lanes: 2 x 4 values a token.  Adding each over 64 lanes would take
+// more instructions than all the rest (6 each).  Pairs of values are added over half of the lanes instead, one value left in
+// either half (two instructions a pair with the swaps of 32 and 16 lanes), so that the number of values halves with the
+// lanes they still have to be added over: 2.2 instructions a value, and at the end lane l of a wave has the sum of
+// value l of 64 (8 tokens, 4 states, B and C).  Channel blocks meet in a second kernel, in the same order on every call.
+#include "scan_kernel.h"
+
+namespace dconv {
+
+namespace {
+
+__device__ __forceinline__ unsigned bits(float v) { return __builtin_bit_cast(unsigned, v); }
+__device__ __forceinline__ float value(unsigned v) { return __builtin_bit_cast(float, v); }
+
+// lanes 0..31: a over lanes l, l + 32; lanes 32..63: b
+__device__ __forceinline__ float fold32(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(bits(a), bits(b), false, false);
+    return value(r[0]) + value(r[1]);
+}
+
+// lanes with bit 4 clear: a over l, l + 16; set: b
+__device__ __forceinline__ float fold16(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(bits(a), bits(b), false, false);
+    return value(r[0]) + value(r[1]);
+}
+
+// lanes with `upper` clear: a over this lane and its partner by CTRL, whose `upper` is the other one; set: b
+template <int CTRL> __device__ __forceinline__ float fold(float a, float b, bool upper)
+{
+    const float keep = upper ? b : a, give = upper ? a : b;
+    return keep + value(__builtin_amdgcn_update_dpp(0, bits(give), CTRL, 0xf, 0xf, true));
+}
+
+constexpr int kAcross8 = 0x128, kAcross4 = 0x141, kAcross2 = 0x4e, kAcross1 = 0xb1;   // lane bits 3, 2, 1, 0
+
+// What each chunk but the first leaves of g at its start, begun at zero (the last: at the gradient of the call's last
+// state), and its sum of d.
+template <typename T, int W>
+__global__ void __launch_bounds__(kWave * W)
+scan_back_kernel(ScanParams p)
+{
+    constexpr int E = kT / W;
+    __shared__ float2 step[kT][kWave];                  // d, dy
+    ScanPlace a = scan_place(p);
+    a.chunk += 1;
+    a.tile0 += p.chunk_tiles;
+    a.tile1 = min(a.tile0 + p.chunk_tiles, p.tiles);
+    a.stop = max(a.tile0, min(a.tile1, (a.len + kT - 1) / kT));
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = a.c0 + lane, s0 = wave * kR;
+    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = a.nc - tc, ec = a.c0 + tc;
+    float A[kR], carry[kR] = {}, dtotal = 0.f, dbias[E] = {};
+    load_states(p.A + (int64_t)c * p.S, s0, p.S, lane < a.nc, A);
+#pragma unroll
+    for (int r = 0; r < kR; ++r) A[r] *= kLog2e;
+    if (a.chunk == p.chunks - 1 && p.dstate_out)
+        load_states(p.dstate_out + ((int64_t)a.n * p.C + c) * p.S, s0, p.S, lane < a.nc, carry);
+    if (nv > 0 && p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
+    for (int tile = a.stop - 1; tile >= a.tile0; --tile) {
+        const int t = tile * kT + tt;
+        const bool in = t < a.len && nv > 0;
+        float dl[E] = {}, dy[E] = {}, z[E];
+        if (in) {
+            load_some<E>(p.delta.at<const T>(a.n, t, ec), nv, dl);
+            load_some<E>(p.dout.at<const T>(a.n, t, ec), nv, dy);
+            if (p.z.p) {
+                load_some<E>(p.z.at<const T>(a.n, t, ec), nv, z);
+#pragma unroll
+                for (int i = 0; i < E; ++i) dy[i] *= z[i] * sigmoid(z[i]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float raw = dl[i] + dbias[i];
+            step[tt][tc + i] = make_float2(in && i < nv ? (p.softplus ? softplus(raw) : raw) : 0.f, in && i < nv ? dy[i] : 0.f);
+        }
+        __syncthreads();
+        bc_ptr bc = bc_of(p, a, W, wave) + (int64_t)tile * kT * W;
+#pragma unroll
+        for (int k = kT - 1; k >= 0; --k) {
+            const float2 d = step[k][lane];
+            const f8 v = bc[k * W];
+#pragma unroll
+            for (int r = 0; r < kR; ++r) carry[r] = exp2_(d.x * A[r]) * __builtin_fmaf(v[kR + r], d.y, carry[r]);
+            dtotal += d.x;
+        }
+    }
+    const int64_t row = (int64_t)a.n * p.chunks + a.chunk;
+    store_states(p.back + lane_states(p, a, row, W, wave, lane), carry);
+    if (wave == 0) p.dsum[(row * p.blocks + a.block) * kWave + lane] = dtotal;
+}
+
+template <typename T, int W>
+__global__ void __launch_bounds__(kWave * W, 2)
+scan_grad_kernel(ScanParams p)
+{
+    constexpr int E = kT / W;
+    __shared__ float2 step[kT][kWave];                  // d, d u
+    __shared__ float gout[kT][kWave];                   // dy
+    __shared__ float sums[3][W][kT][kWave];             // over a wave's states: C h, g B, e A
+    const ScanPlace a = scan_place(p);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = a.c0 + lane, s0 = wave * kR;
+    const bool ok = lane < a.nc, gate = p.z.p != nullptr;
+    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = a.nc - tc, ec = a.c0 + tc;
+
+    float A[kR], carry[kR] = {}, dA[kR] = {};
+    load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
+    const int64_t own = ((int64_t)a.n * p.C + c) * p.S, row = (int64_t)a.n * p.chunks;
+    if (a.chunk == p.chunks - 1) {
+        if (p.dstate_out) load_states(p.dstate_out + own, s0, p.S, ok, carry);
+    } else {
+        for (int k = p.chunks - 1; k > a.chunk; --k) {
+            float e[kR];
+            load_states(p.back + lane_states(p, a, row + k, W, wave, lane), e);
+            const float d = p.dsum[((row + k) * p.blocks + a.block) * kWave + lane];
+#pragma unroll
+            for (int r = 0; r < kR; ++r) carry[r] = __builtin_fmaf(exp2_(d * (A[r] * kLog2e)), carry[r], e[r]);
+        }
+    }
+    float dbias[E] = {}, skip[E] = {}, sumD[E] = {}, sumB[E] = {};
+    if (nv > 0) {
+        if (p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
+        if (p.D) load_some<E>(p.D + ec, nv, skip);
+        const float zero[E] = {};
+        for (int tile = a.stop; tile < a.tile1; ++tile) {            // tiles that do not count
+            const int t = tile * kT + tt;
+            if (t >= p.L) continue;
+            store_some<E>(p.du.at<T>(a.n, t, ec), nv, zero);
+            store_some<E>(p.ddelta.at<T>(a.n, t, ec), nv, zero);
+            if (gate) store_some<E>(p.dz.at<T>(a.n, t, ec), nv, zero);
+        }
+    }
+    for (int tile = a.stop - 1; tile >= a.tile0; --tile) {
+        const int t = tile * kT + tt;
+        const bool in = t < a.len && nv > 0;
+        float u[E] = {}, dl[E] = {}, go[E] = {}, z[E] = {}, d[E];
+        if (in) {
+            load_some<E>(p.u.at<const T>(a.n, t, ec), nv, u);
+            load_some<E>(p.delta.at<const T>(a.n, t, ec), nv, dl);
+            load_some<E>(p.dout.at<const T>(a.n, t, ec), nv, go);
+            if (gate) load_some<E>(p.z.at<const T>(a.n, t, ec), nv, z);
+        }
+        float h0[kR];
+        load_states(p.starts + lane_states(p, a, (int64_t)a.n * p.tiles + tile, W, wave, lane), h0);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float raw = dl[i] + dbias[i];
+            d[i] = in && i < nv ? (p.softplus ? softplus(raw) : raw) : 0.f;
+            step[tt][tc + i] = make_float2(d[i], d[i] * u[i]);
+            gout[tt][tc + i] = gate ? go[i] * z[i] * sigmoid(z[i]) : go[i];
+        }
+        __syncthreads();
+        bc_ptr bc = bc_of(p, a, W, wave) + (int64_t)tile * kT * W;
+        float dec[kT][kR], h[kT][kR];
+#pragma unroll
+        for (int k = 0; k < kT; ++k) {
+            const float2 s = step[k][lane];
+            const f8 v = bc[k * W];
+            float y = 0.f;
+#pragma unroll
+            for (int r = 0; r < kR; ++r) {
+                dec[k][r] = exp2_(s.x * (A[r] * kLog2e));
+                h[k][r] = __builtin_fmaf(dec[k][r], k ? h[k - 1][r] : h0[r], s.y * v[r]);
+                y = r ? __builtin_fmaf(v[kR + r], h[k][r], y) : v[kR + r] * h[k][r];
+            }
+            if (gate) sums[0][wave][k][lane] = y;
+        }
+        float packed[8];
+#pragma unroll
+        for (int k = kT - 1; k >= 0; --k) {
+            const float2 s = step[k][lane];
+            const float dy = gout[k][lane];
+            const f8 v = bc[k * W];
+            float q = 0.f, ea = 0.f, pair[kR];
+#pragma unroll
+            for (int r = 0; r < kR; ++r) {
+                const float g = __builtin_fmaf(v[kR + r], dy, carry[r]);
+                carry[r] = g * dec[k][r];
+                const float e = carry[r] * (k ? h[k - 1][r] : h0[r]);
+                q = r ? __builtin_fmaf(g, v[r], q) : g * v[r];
+                ea = r ? __builtin_fmaf(e, A[r], ea) : e * A[r];
+                dA[r] = __builtin_fmaf(e, s.x, dA[r]);
+                pair[r] = fold32(g * s.y, dy * h[k][r]);
+            }
+            sums[1][wave][k][lane] = q;
+            sums[2][wave][k][lane] = ea;
+            packed[k & 7] = fold<kAcross8>(fold16(pair[0], pair[2]), fold16(pair[1], pair[3]), lane & 8);
+            if ((k & 7) == 0) {
+                float f[4], e[2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[i] = fold<kAcross4>(packed[i], packed[i + 4], lane & 4);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) e[i] = fold<kAcross2>(f[i], f[i + 2], lane & 2);
+                const int64_t at = (((int64_t)a.block * p.N + a.n) * p.tiles + tile) * 2 + k / 8;
+                p.part_bc[(at * W + wave) * kWave + lane] = fold<kAcross1>(e[0], e[1], lane & 1);
+            }
+        }
+        __syncthreads();
+        if (nv > 0 && t < p.L) {
+            float du[E], dd[E], dz[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                float y = skip[i] * u[i], q = 0.f, ea = 0.f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    if (gate) y += sums[0][w][tt][tc + i];
+                    q += sums[1][w][tt][tc + i];
+                    ea += sums[2][w][tt][tc + i];
+                }
+                const float sg = sigmoid(z[i]), dy = gate ? go[i] * z[i] * sg : go[i];
+                du[i] = __builtin_fmaf(d[i], q, skip[i] * dy);
+                dd[i] = __builtin_fmaf(u[i], q, ea);
+                if (p.softplus) dd[i] *= sigmoid(dl[i] + dbias[i]);
+                dz[i] = go[i] * y * (sg * (1.f + z[i] * (1.f - sg)));
+                if (!in) du[i] = dd[i] = dz[i] = 0.f;
+                sumD[i] = __builtin_fmaf(dy, u[i], sumD[i]);
+                sumB[i] += dd[i];
+            }
+            store_some<E>(p.du.at<T>(a.n, t, ec), nv, du);
+            store_some<E>(p.ddelta.at<T>(a.n, t, ec), nv, dd);
+            if (gate) store_some<E>(p.dz.at<T>(a.n, t, ec), nv, dz);
+        }
+    }
+    if (a.chunk == 0 && p.dstate && ok) store_some<kR>(p.dstate + own + s0, p.S - s0, carry);
+    store_states(p.part_A + lane_states(p, a, row + a.chunk, W, wave, lane), dA);
+    // dD and the gradient of the bias: over the sixteen tokens of a tile
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < E; ++i) step[tt][tc + i] = make_float2(sumD[i], sumB[i]);
+    __syncthreads();
+    if (wave == 0) {
+        float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kT; ++k) {
+            s.x += step[k][lane].x;
+            s.y += step[k][lane].y;
+        }
+        const int64_t at = ((row + a.chunk) * p.blocks + a.block) * kWave + lane;
+        p.part_D[at] = s.x;
+        p.part_bias[at] = s.y;
+    }
+}
+
+// dB and dC of 64 values (8 tokens, 4 states) from the parts of a group's channel blocks.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+scan_sum_bc_kernel(const float* part, Rows dB, Rows dC, int64_t b_g, int64_t c_g, const int* lengths, int N, int L, int G, int S,
+                   int W, int tiles, int gblocks)
+{
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int lane = (int)(i & 63);
+    const int64_t unit = i >> 6, per = (int64_t)tiles * 2 * W;             // a wave's share: [G][N][tiles][2][W]
+    const int64_t seq = unit / per, in = unit - seq * per;
+    const int g = (int)(seq / N), n = (int)(seq - (int64_t)g * N);
+    if (g >= G) return;
+    const int w = (int)(in % W);
+    const int t = (int)(in / W) * 8 + (lane & 7), s = w * kR + (lane >> 4 & 1) * 2 + (lane >> 3 & 1);
+    if (t >= L || s >= S) return;
+    float v = 0.f;
+    if (t < length_of(lengths, n, L))
+        for (int k = 0; k < gblocks; ++k) v += part[(((int64_t)(g * gblocks + k) * N + n) * per + in) * kWave + lane];
+    if (lane < 32) dB.at<T>(n, t, 0)[g * b_g + s] = (T)v;
+    else dC.at<T>(n, t, 0)[g * c_g + s] = (T)v;
+}
+
+// dA, dD and the gradient of the bias from the parts of all sequences and chunks.
+__global__ void __launch_bounds__(kWave)
+scan_sum_kernel(ScanParams p, int W, float* dA, float* dD, float* dbias)
+{
+    const int lane = threadIdx.x, block = blockIdx.x / (W + 1), w = blockIdx.x - block * (W + 1);
+    const int g = block / p.gblocks, k = block - g * p.gblocks, c = g * p.group + k * kWave + lane;
+    const bool ok = k * kWave + lane < p.group;
+    const int64_t rows = (int64_t)p.N * p.chunks;
+    if (w < W) {
+        float s[kR] = {};
+        for (int64_t r = 0; r < rows; ++r) {
+            float v[kR];
+            load_states(p.part_A + (((r * p.blocks + block) * W + w) * kWave + lane) * kR, v);
+            for (int i = 0; i < kR; ++i) s[i] += v[i];
+        }
+        if (ok) store_some<kR>(dA + (int64_t)c * p.S + w * kR, p.S - w * kR, s);
+        return;
+    }
+    float d = 0.f, b = 0.f;
+    for (int64_t r = 0; r < rows; ++r) {
+        d += p.part_D[(r * p.blocks + block) * kWave + lane];
+        b += p.part_bias[(r * p.blocks + block) * kWave + lane];
+    }
+    if (ok && dD) dD[c] = d;
+    if (ok && dbias) dbias[c] = b;
+}
+
+template <typename T, int W> void launch_kernels(const ScanParams& p, hipStream_t st)
+{
+    if (p.chunks > 1)
+        hipLaunchKernelGGL((scan_back_kernel<T, W>), dim3((unsigned)(p.total - (int64_t)p.N * p.blocks)), dim3(kWave * W), 0, st, p);
+    hipLaunchKernelGGL((scan_grad_kernel<T, W>), dim3((unsigned)p.total), dim3(kWave * W), 0, st, p);
+}
+
+template <typename T> void launch_typed(const dconv_scan_args& a, const ScanParams& p, int W, hipStream_t st)
+{
+    switch (W) {
+    case 1: launch_kernels<T, 1>(p, st); break;
+    case 2: launch_kernels<T, 2>(p, st); break;
+    case 4: launch_kernels<T, 4>(p, st); break;
+    default: launch_kernels<T, 8>(p, st); break;
+    }
+    const int64_t n = (int64_t)p.N * p.G * p.tiles * 2 * W * kWave;
+    hipLaunchKernelGGL((scan_sum_bc_kernel<T>), dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p.part_bc,
+                       Rows{a.dB.p, a.dB.sn, a.dB.sl}, Rows{a.dC.p, a.dC.sn, a.dC.sl}, a.dB.sg, a.dC.sg, a.lengths, a.N, a.L,
+                       a.G, a.S, W, p.tiles, p.gblocks);
+}
+
+// The workspace of a gradient call, in floats: where its parts begin, and how many there are.
+struct GradSpace { int64_t ends, back, dsum, bc_parts, A_parts, D_parts, bias_parts, starts, all; };
+
+GradSpace space_of(const dconv_scan_args& a, const ScanPlan& pl)
+{
+    const int64_t rows = (int64_t)a.N * pl.chunks * pl.blocks * kWave, states = rows * pl.waves * kR;
+    GradSpace s;
+    int64_t at = scan_bc_floats(a, pl);
+    auto take = [&](int64_t n) { const int64_t here = at; at += (n + 3) / 4 * 4; return here; };
+    s.ends = take(pl.chunks > 1 ? states : 0);
+    s.back = take(pl.chunks > 1 ? states : 0);
+    s.dsum = take(pl.chunks > 1 ? rows : 0);
+    s.bc_parts = take((int64_t)pl.blocks * a.N * pl.tiles * 2 * pl.waves * kWave);
+    s.A_parts = take(states);
+    s.D_parts = take(rows);
+    s.bias_parts = take(rows);
+    s.starts = take(a.starts ? 0 : scan_starts_floats(a));
+    s.all = at;
+    return s;
+}
+
+}  // namespace
+
+}  // namespace dconv
+
+using namespace dconv;
+
+extern "C" {
+
+long long dconv_scan_workspace(const dconv_scan_args* a, int grad)
+{
+    if (!a || !token_bytes(a->dtype) || !scan_sizes_ok(*a)) return -1;
+    const ScanPlan pl = scan_plan(*a, grad != 0);
+    return 4 * (grad ? space_of(*a, pl).all : scan_bc_floats(*a, pl) + scan_chunk_floats(*a, pl));
+}
+
+int dconv_scan_grad(const dconv_scan_args* a, void* stream)
+{
+    int rc = scan_check(a, 1);
+    if (rc != DCONV_OK) return rc;
+    const hipStream_t st = (hipStream_t)stream;
+    const ScanPlan pl = scan_plan(*a, true);
+    const GradSpace s = space_of(*a, pl);
+    float* ws = (float*)a->workspace;
+    ScanParams p = scan_params(*a, pl);
+    p.bc = ws;
+    p.ends = ws + s.ends; p.back = ws + s.back; p.dsum = ws + s.dsum;
+    p.part_bc = ws + s.bc_parts; p.part_A = ws + s.A_parts; p.part_D = ws + s.D_parts; p.part_bias = ws + s.bias_parts;
+    rc = launch_scan_bc(*a, pl, ws, st);
+    if (rc != DCONV_OK) return rc;
+    if (!a->starts) {
+        p.starts = ws + s.starts;
+        ScanParams forward = p;
+        forward.state_out = nullptr;
+        rc = launch_scan_forward(*a, forward, pl, false, st);
+        if (rc != DCONV_OK) return rc;
+    }
+    begin_launch();
+    if (a->dtype == DCONV_DTYPE_F16) launch_typed<_Float16>(*a, p, pl.waves, st);
+    else if (a->dtype == DCONV_DTYPE_BF16) launch_typed<__bf16>(*a, p, pl.waves, st);
+    else launch_typed<float>(*a, p, pl.waves, st);
+    hipLaunchKernelGGL(scan_sum_kernel, dim3((unsigned)(pl.blocks * (pl.waves + 1))), dim3(kWave), 0, st, p, pl.waves, a->dA, a->dD,
+                       a->ddelta_bias);
+    return launch_status();
+}
+
+}  // extern "C"

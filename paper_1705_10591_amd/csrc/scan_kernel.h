@@ -1,0 +1,125 @@
+// The scan over tokens, what its forms share: h[t] = exp(d[t] A) h[t-1] + d[t] u[t] B[t] for every channel and state.
+//
+// The recurrence is elementwise, so the work goes to the vector ALU: a product, an exponential, a product and two
+// multiply-adds for each (token, channel, state).  What shapes the kernels:
+//  * A lane is a channel and a wave has kR = 4 states of 64 channels: B[t] and C[t] are then the same for a whole wave and
+//    come through scalar registers, which costs the vector ALU nothing.  The W = S / 4 waves of a workgroup have the other
+//    states of the same channels; what all states of a channel share (d, d u, the sum over states) goes through LDS.
+//  * Tokens come in tiles of kT = 16.  Thread by thread a tile's 16 x 64 values are loaded and stored in runs of E = 16 / W
+//    channels, and d, its softplus and the gate are computed once, not once per wave.
+//  * bc_kernel lays B and C out for the scalar loads first: fp32, [N][G][tokens][W][4 of B, 4 of C], zeros behind the end
+//    of a sequence and beyond state S.  With d = 0 there too, tokens that do not count leave the state as it is, and
+//    the loops need no masks.
+//  * A call with too few (sequence, channel block) pairs for the chip cuts its sequences into chunks: a first launch
+//    runs each chunk from a state of zero, and each workgroup of the second begins by putting together what the chunks
+//    before it leave, since a chunk changes the state it is given by the factor exp(A sum d) alone.
+#pragma once
+#include "tokens.h"
+
+namespace dconv {
+
+constexpr int kT = 16;               // tokens of a tile
+constexpr int kR = 4;                // states of a wave
+constexpr int kMaxStates = 32;       // eight waves
+
+typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f8 __attribute__((ext_vector_type(8), aligned(16)));
+typedef const __attribute__((address_space(4))) f8* bc_ptr;        // constant memory: scalar loads
+
+struct Rows {                        // a token tensor: base, elements between sequences and tokens
+    void* p;
+    int64_t n, l;
+    template <typename T> __device__ __forceinline__ T* at(int seq, int64_t t, int c) const
+    {
+        return (T*)p + seq * n + t * l + c;
+    }
+};
+
+struct ScanParams {
+    Rows u, delta, z, out, dout, du, ddelta, dz;
+    const float *A, *D, *delta_bias, *state, *dstate_out;
+    float *state_out, *dstate, *starts;
+    const int* lengths;
+    const float* bc;
+    float *ends, *dsum;              // of the chunks: states [N][chunks][blocks][W][64][4], sums of d [N][chunks][blocks][64]
+    float *back;                     // ... and of the way back, laid out like ends
+    float *part_bc;                  // gradients of B and C: [blocks][N][tiles][2][W][64]
+    float *part_A, *part_D, *part_bias;   // [N][chunks][blocks][W][64][4], [N][chunks][blocks][64]
+    int N, L, C, S, G, softplus;
+    int group, gblocks, blocks;      // channels of a group, its blocks of 64, all blocks
+    int tiles, chunk_tiles, chunks;  // of L tokens
+    int64_t total;                   // workgroups
+};
+
+// What a workgroup works on.
+struct ScanPlace {
+    int n, chunk, block, g, c0, nc;  // sequence, chunk, channel block; group, first channel, channels of the block
+    int len, tile0, tile1, stop;     // the sequence's tokens; the chunk's tiles, those with tokens that count end at stop
+};
+
+__device__ __forceinline__ ScanPlace scan_place(const ScanParams& p)
+{
+    ScanPlace a;
+    const unsigned b = blockIdx.x, r = b / (unsigned)p.blocks;
+    a.block = b - r * p.blocks;
+    a.chunk = r / (unsigned)p.N;
+    a.n = r - a.chunk * p.N;
+    a.g = a.block / p.gblocks;
+    const int k = a.block - a.g * p.gblocks;
+    a.c0 = a.g * p.group + k * kWave;
+    a.nc = min(kWave, p.group - k * kWave);
+    a.len = length_of(p.lengths, a.n, p.L);
+    a.tile0 = a.chunk * p.chunk_tiles;
+    a.tile1 = min(a.tile0 + p.chunk_tiles, p.tiles);
+    a.stop = max(a.tile0, min(a.tile1, (a.len + kT - 1) / kT));
+    return a;
+}
+
+__device__ __forceinline__ bc_ptr bc_of(const ScanParams& p, const ScanPlace& a, int W, int wave)
+{
+    return (bc_ptr)(p.bc) + ((int64_t)a.n * p.G + a.g) * p.tiles * kT * W + wave;
+}
+
+// Index of this lane's four states among those of all channels.
+__device__ __forceinline__ int64_t lane_states(const ScanParams& p, const ScanPlace& a, int64_t row, int W, int wave, int lane)
+{
+    return (((row * p.blocks + a.block) * W + wave) * kWave + lane) * kR;
+}
+
+// Four states of a channel in a user's [C][S], of which those beyond S are 0.
+__device__ __forceinline__ void load_states(const float* p, int s0, int S, bool ok, float (&v)[kR])
+{
+#pragma unroll
+    for (int r = 0; r < kR; ++r) v[r] = 0.f;
+    if (ok) load_some<kR>(p + s0, S - s0, v);
+}
+
+__device__ __forceinline__ void load_states(const float* p, float (&v)[kR])
+{
+    const f4 t = *(const f4*)p;
+#pragma unroll
+    for (int r = 0; r < kR; ++r) v[r] = t[r];
+}
+
+__device__ __forceinline__ void store_states(float* p, const float (&v)[kR])
+{
+    f4 t;
+#pragma unroll
+    for (int r = 0; r < kR; ++r) t[r] = v[r];
+    *(f4*)p = t;
+}
+
+// host side (scan.hip)
+int scan_waves(int S);
+bool scan_sizes_ok(const dconv_scan_args& a);
+int scan_check(const dconv_scan_args* a, int form);        // 0 prompt, 1 gradient, 2 step
+struct ScanPlan { int waves, group, gblocks, blocks, tiles, chunks, chunk_tiles; };
+ScanPlan scan_plan(const dconv_scan_args& a, bool grad);
+ScanParams scan_params(const dconv_scan_args& a, const ScanPlan& pl);
+int64_t scan_bc_floats(const dconv_scan_args& a, const ScanPlan& pl);
+int64_t scan_chunk_floats(const dconv_scan_args& a, const ScanPlan& pl);      // ends and dsum
+int64_t scan_starts_floats(const dconv_scan_args& a);
+int launch_scan_bc(const dconv_scan_args& a, const ScanPlan& pl, float* bc, hipStream_t st);
+int launch_scan_forward(const dconv_scan_args& a, ScanParams p, const ScanPlan& pl, bool out, hipStream_t st);
+
+}  // namespace dconv

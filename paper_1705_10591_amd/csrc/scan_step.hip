@@ -1,0 +1,101 @@
+// The scan for one token of each row: h = exp(d A) h + d u B in a cache of states, y = sum_s C h + D u, gated.
+//
+// Bound by the states, 4 bytes read and 4 written for each; small calls by the latency of one chain of loads.  A lane
+// has four states of a channel (16 bytes of the cache), W lanes a channel; they add y up among themselves.
+#include "scan_kernel.h"
+
+namespace dconv {
+
+namespace {
+
+struct StepParams {
+    Rows u, delta, z, out, B, Cm;
+    int64_t b_g, c_g;
+    const float *A, *D, *delta_bias;
+    float* state;
+    const int* slots;
+    int M, C, S, group, cblocks, softplus;
+};
+
+template <int CTRL> __device__ __forceinline__ float add_lane(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+
+template <typename T, int W>
+__global__ void __launch_bounds__(kThreads)
+scan_step_kernel(StepParams p)
+{
+    const int n = blockIdx.x / p.cblocks;
+    const int slot = slot_of(p.slots, n, p.M);
+    const int c = (blockIdx.x - n * p.cblocks) * (kThreads / W) + threadIdx.x / W, q = threadIdx.x % W, s0 = q * kR;
+    if (c >= p.C) return;                                    // (all lanes of a channel together)
+    T* out = p.out.at<T>(n, 0, c);
+    if (slot < 0) {
+        if (q == 0) *out = (T)0.f;
+        return;
+    }
+    float A[kR], b[kR], cm[kR], h[kR];
+    const int g = c / p.group;
+    float* st = p.state + ((int64_t)slot * p.C + c) * p.S + s0;
+    load_some<kR>(st, p.S - s0, h);
+    load_some<kR>(p.A + (int64_t)c * p.S + s0, p.S - s0, A);
+    load_some<kR>(p.B.at<const T>(n, 0, 0) + g * p.b_g + s0, p.S - s0, b);
+    load_some<kR>(p.Cm.at<const T>(n, 0, 0) + g * p.c_g + s0, p.S - s0, cm);
+    const float u = (float)*p.u.at<const T>(n, 0, c);
+    const float raw = (float)*p.delta.at<const T>(n, 0, c) + (p.delta_bias ? p.delta_bias[c] : 0.f);
+    const float z = p.z.p ? (float)*p.z.at<const T>(n, 0, c) : 0.f, skip = p.D ? p.D[c] : 0.f;
+    const float d = p.softplus ? softplus(raw) : raw, du = d * u;
+    float y = 0.f;
+#pragma unroll
+    for (int r = 0; r < kR; ++r) {
+        h[r] = __builtin_fmaf(exp2_(d * (A[r] * kLog2e)), h[r], du * b[r]);
+        y = __builtin_fmaf(cm[r], h[r], y);
+    }
+    store_some<kR>(st, p.S - s0, h);
+    if (W > 1) y = add_lane<0xb1>(y);                        // the lane beside
+    if (W > 2) y = add_lane<0x4e>(y);                        // ... two further
+    if (W > 4) y = add_lane<0x141>(y);                       // ... in the other half of eight
+    y = __builtin_fmaf(skip, u, y);
+    if (p.z.p) y *= z * sigmoid(z);
+    if (q == 0) *out = (T)y;
+}
+
+template <typename T> void launch_typed(const StepParams& p, int W, int64_t blocks, hipStream_t st)
+{
+    const dim3 grid((unsigned)blocks), threads(kThreads);
+    switch (W) {
+    case 1: hipLaunchKernelGGL((scan_step_kernel<T, 1>), grid, threads, 0, st, p); break;
+    case 2: hipLaunchKernelGGL((scan_step_kernel<T, 2>), grid, threads, 0, st, p); break;
+    case 4: hipLaunchKernelGGL((scan_step_kernel<T, 4>), grid, threads, 0, st, p); break;
+    default: hipLaunchKernelGGL((scan_step_kernel<T, 8>), grid, threads, 0, st, p); break;
+    }
+}
+
+}  // namespace
+
+}  // namespace dconv
+
+using namespace dconv;
+
+extern "C" int dconv_scan_step(const dconv_scan_args* a, void* stream)
+{
+    const int rc = scan_check(a, 2);
+    if (rc != DCONV_OK) return rc;
+    StepParams p{};
+    auto rows = [](const dconv_tokens& t) { return Rows{t.p, t.sn, t.sl}; };
+    p.u = rows(a->u); p.delta = rows(a->delta); p.z = rows(a->z); p.out = rows(a->out); p.B = rows(a->B); p.Cm = rows(a->Cm);
+    p.b_g = a->B.sg; p.c_g = a->Cm.sg;
+    p.A = a->A; p.D = a->D; p.delta_bias = a->delta_bias; p.state = a->state_out; p.slots = a->slots;
+    p.M = a->M; p.C = a->C; p.S = a->S; p.group = a->C / a->G; p.softplus = a->softplus;
+    const int W = scan_waves(a->S);
+    p.cblocks = (a->C - 1) / (kThreads / W) + 1;
+    const int64_t blocks = (int64_t)a->N * p.cblocks;
+    if (blocks > 2147483647LL) return DCONV_BAD_SHAPE;
+    const hipStream_t st = (hipStream_t)stream;
+    begin_launch();
+    if (a->dtype == DCONV_DTYPE_F16) launch_typed<_Float16>(p, W, blocks, st);
+    else if (a->dtype == DCONV_DTYPE_BF16) launch_typed<__bf16>(p, W, blocks, st);
+    else launch_typed<float>(p, W, blocks, st);
+    return launch_status();
+}

@@ -1,0 +1,100 @@
+// What the operators over tokens (causal.hip, scan*.hip) share: element types, runs of channels, activations.
+#pragma once
+#include "common.h"
+
+namespace dconv {
+
+template <int N> using vf = float __attribute__((ext_vector_type(N)));
+
+// N elements that lie next to each other, as fp32.  The hardware takes loads and stores of up to 16 bytes at any address
+// (an odd number of channels moves every other row off its alignment), so that there is one kernel for all alignments.
+template <int N, typename T> __device__ __forceinline__ void load_run(const T* p, float (&v)[N])
+{
+    typedef T vt __attribute__((ext_vector_type(N)));
+    vt t;
+    __builtin_memcpy(&t, p, sizeof(T) * N);
+    for (int i = 0; i < N; ++i) v[i] = (float)t[i];
+}
+template <typename T> __device__ __forceinline__ void load_run(const T* p, float (&v)[1]) { v[0] = (float)p[0]; }
+
+template <int N, typename T> __device__ __forceinline__ void store_run(T* p, const float (&v)[N])
+{
+    typedef T vt __attribute__((ext_vector_type(N)));
+    vt t;
+    for (int i = 0; i < N; ++i) t[i] = (T)v[i];           // round to nearest even
+    __builtin_memcpy(p, &t, sizeof(T) * N);
+}
+template <typename T> __device__ __forceinline__ void store_run(T* p, const float (&v)[1]) { p[0] = (T)v[0]; }
+
+// ... of which only the first n exist (the others read as 0 and are not written)
+template <int N, typename T> __device__ __forceinline__ void load_some(const T* p, int n, float (&v)[N])
+{
+    if (n >= N) {
+        load_run(p, v);
+    } else {
+        for (int i = 0; i < N; ++i) v[i] = i < n ? (float)p[i] : 0.f;
+    }
+}
+template <int N, typename T> __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[N])
+{
+    if (n >= N) {
+        store_run(p, v);
+    } else {
+        for (int i = 0; i < N; ++i)
+            if (i < n) p[i] = (T)v[i];
+    }
+}
+
+constexpr int kMaxTokens = 1 << 30;      // of a sequence: token numbers and what is added to them fit 32 bits
+constexpr double kMaxElements = 1.1e18; // of a tensor, 2^60: sizes in 64 bits do not overflow
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float rcp_(float x) { return __builtin_amdgcn_rcpf(x); }
+
+// 1 / (1 + e^-x): exp2 and the reciprocal are good to 1 ulp each, and where e^-x overflows the quotient is 0 as it should be.
+__device__ __forceinline__ float sigmoid(float x) { return rcp_(1.f + exp2_(-kLog2e * x)); }
+
+// log(1 + e^x).  log(w) loses the digits that w = 1 + e rounded away; e * log(w) / (w - 1) has them back, since the
+// quotient log(w) / (w - 1) changes slowly (Goldberg, "What every computer scientist should know about floating-point
+// arithmetic", theorem 4).  Beyond 20 the sum is x to within 2e-9.
+__device__ __forceinline__ float softplus(float x)
+{
+    const float e = exp2_(kLog2e * x), w = 1.f + e;
+    const float r = w == 1.f ? e : e * (kLn2 * __builtin_amdgcn_logf(w)) * rcp_(w - 1.f);
+    return x > 20.f ? x : r;
+}
+
+// Tokens of sequence n that count.
+__device__ __forceinline__ int length_of(const int* lengths, int n, int L)
+{
+    return lengths ? min(max(lengths[n], 0), L) : L;
+}
+
+// The row of a cache of M that row n of a step works on, -1 for padding: slots outside the cache, and those that an earlier
+// row has named.  All threads of a workgroup call it with the same n.
+__device__ __forceinline__ int slot_of(const int* slots, int n, int M)
+{
+    if (!slots) return n;
+    const int s = slots[n];
+    int twice = 0;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) twice |= slots[i] == s;
+    return __syncthreads_or(twice) || s < 0 || s >= M ? -1 : s;
+}
+
+// Workgroups go round the eight XCDs in turn, each with an L2 of its own: neighbours that share rows get numbers that
+// are eight apart.
+__device__ __forceinline__ int64_t near_block(int64_t b, int64_t total)
+{
+    const int64_t each = total >> 3, rest = total & 7, x = b & 7, i = b >> 3;
+    return x * each + (x < rest ? x : rest) + i;
+}
+
+inline bool aligned_to(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+inline int token_bytes(int dtype)
+{
+    return dtype == DCONV_DTYPE_F32 ? 4 : dtype == DCONV_DTYPE_F16 || dtype == DCONV_DTYPE_BF16 ? 2 : 0;
+}
+
+}  // namespace dconv

@@ -1,0 +1,342 @@
+"""Operators over the tokens of sequences: the short causal convolution and the selective scan (dconv.h says what they compute).
+
+Token tensors are [N, L, C] (B and C of the scan [N, L, G, S]) with the last dimension contiguous and any strides before
+it; a step has no L.  As everywhere in this package, functions check and marshal arguments, enqueue on the current stream
+of the tensors' device and return; outputs that are not passed in, and workspaces, come from torch's allocator, which
+is safe for streams and captured graphs.  Gradients are explicit calls: nothing is recorded for torch.autograd.
+"""
+from __future__ import annotations
+
+import ctypes
+import struct
+from typing import NamedTuple, Optional
+
+import torch
+
+EXPORTS = ("dconv_causal", "dconv_causal_grad", "dconv_causal_step", "dconv_causal_workspace",
+           "dconv_scan", "dconv_scan_grad", "dconv_scan_step", "dconv_scan_workspace", "dconv_scan_starts")
+DTYPE_F32 = 3
+_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: DTYPE_F32}
+
+# The argument structs of dconv.h, packed at once: filling a ctypes structure field by field takes several times as long
+# as a single token takes the GPU.
+_CAUSAL = struct.Struct("8i" + 4 * "4q" + "12q")
+_SCAN = struct.Struct("8i" + 12 * "4q" + "15q")
+_NONE = (0, 0, 0, 0)
+
+
+def declare(lib: ctypes.CDLL) -> None:
+    for name in EXPORTS:
+        fn = getattr(lib, name)
+        if name.endswith(("_workspace", "_starts")):
+            fn.argtypes = [ctypes.c_char_p] + ([ctypes.c_int] if name == "dconv_scan_workspace" else [])
+            fn.restype = ctypes.c_longlong
+        else:
+            fn.argtypes = [ctypes.c_char_p, ctypes.c_void_p]
+            fn.restype = ctypes.c_int
+
+
+def _lib():
+    from . import load_library
+    return load_library()
+
+
+def _run(fn, index, args):
+    from . import _enqueue
+    _enqueue(fn, index, args)
+
+
+def _first(t, dims, what):
+    """Type, device and sizes that the other tensors of a call have to agree with."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _DTYPES and t.dim() == dims):
+        raise TypeError(f"{what} must be a float16, bfloat16 or float32 CUDA tensor with {dims} dims")
+    if 0 in t.shape:
+        from . import STATUS_BAD_SHAPE, _raise
+        _raise(STATUS_BAD_SHAPE)
+    return t.dtype, t.get_device()
+
+
+def _like(t, shape, dtype, index, what):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
+        raise TypeError(f"{what} must be a CUDA tensor of type {dtype}")
+    if t.get_device() != index:
+        raise ValueError(f"{what} is on another device")
+    if t.shape != shape:
+        raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+
+
+def _rows(t, shape, dtype, index, what, out=False):
+    """(pointer, strides of sequence, token and group) of a token tensor."""
+    if t is None:
+        return _NONE
+    _like(t, shape, dtype, index, what)
+    s = t.stride()
+    if s[-1] != 1 and shape[-1] != 1:
+        raise TypeError(f"the last dimension of {what} must be contiguous")
+    strides = {2: (s[0], 0, 0), 3: (s[0], s[1], 0), 4: s[:3]}[len(shape)]
+    if out:
+        # tokens that share memory would be written by several workgroups
+        span = shape[-1]
+        for stride, size in sorted(zip(s[:-1], shape[:-1])):
+            if size > 1:
+                if stride < span:
+                    raise ValueError(f"elements of {what} overlap")
+                span += stride * (size - 1)
+    return (t.data_ptr(), *strides)
+
+
+def _dense(t, shape, dtype, index, what):
+    if t is None:
+        return 0
+    _like(t, shape, dtype, index, what)
+    if not t.is_contiguous():
+        raise TypeError(f"{what} must be contiguous")
+    return t.data_ptr()
+
+
+def _cache(t, tail, dtype, index, what, rows, slots):
+    """(pointer, rows) of a cache of states that a step updates."""
+    if not isinstance(t, torch.Tensor) or t.dim() != len(tail) + 1 or tuple(t.shape[1:]) != tuple(tail):
+        raise ValueError(f"{what} must have the shape (rows, {', '.join(map(str, tail))})")
+    if t.shape[0] == 0 or (slots is None and t.shape[0] < rows):
+        raise ValueError(f"{what} has too few rows")
+    return _dense(t, t.shape, dtype, index, what), t.shape[0]
+
+
+def _workspace(bytes_, index):
+    return torch.empty(max(bytes_, 16), dtype=torch.uint8, device=f"cuda:{index}")
+
+
+class CausalGrad(NamedTuple):
+    """Gradients of dconv_causal: of x (its type), filt and bias (fp32), and of the state where there is one."""
+    dx: torch.Tensor
+    dfilt: torch.Tensor
+    dbias: torch.Tensor
+    dstate: Optional[torch.Tensor]
+
+
+class ScanGrad(NamedTuple):
+    """Gradients of dconv_scan: of the token tensors in their type, of A, D, delta_bias and the state in fp32; None for what
+    the call was not given."""
+    du: torch.Tensor
+    ddelta: torch.Tensor
+    dA: torch.Tensor
+    dB: torch.Tensor
+    dC: torch.Tensor
+    dD: Optional[torch.Tensor]
+    dz: Optional[torch.Tensor]
+    ddelta_bias: Optional[torch.Tensor]
+    dstate: Optional[torch.Tensor]
+
+
+def dconv_causal(x: torch.Tensor, filt: torch.Tensor, bias: torch.Tensor | None = None, *, silu: bool = True,
+                 state: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                 out: torch.Tensor | None = None, state_out: torch.Tensor | None = None) -> torch.Tensor:
+    """out[n,t,c] = act(bias[c] + sum_j filt[c,j] * x[n, t-(F-1)+j, c]), act = silu or nothing.
+
+    x [N,L,C], filt [C,F] (F <= 8), bias [C], all of one type.  state [N,F-1,C]: the rows before token 0 (default: zeros);
+    state_out, which may be `state`, receives the last F-1 rows of each sequence.  lengths [N] int32: the tokens of each
+    sequence that count; out is 0 behind them."""
+    dtype, index = _first(x, 3, "x")
+    N, L, C = x.shape
+    F = _taps(filt, C)
+    if out is None:
+        out = torch.empty((N, L, C), dtype=dtype, device=x.device)
+    rows = (N, F - 1, C)
+    args = _CAUSAL.pack(
+        _DTYPES[dtype], N, L, C, F, 0, bool(silu), 0,
+        *_rows(x, (N, L, C), dtype, index, "x"), *_rows(out, (N, L, C), dtype, index, "out", True), *_NONE, *_NONE,
+        _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
+        _dense(state, rows, dtype, index, "state"), _dense(state_out, rows, dtype, index, "state_out"), 0, 0, 0, 0,
+        _dense(lengths, (N,), torch.int32, index, "lengths"), 0, 0, 0)
+    _run(_lib().dconv_causal, index, args)
+    return out
+
+
+def dconv_causal_grad(dout: torch.Tensor, x: torch.Tensor, filt: torch.Tensor, bias: torch.Tensor | None = None, *,
+                      silu: bool = True, state: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                      dstate_out: torch.Tensor | None = None, dx: torch.Tensor | None = None) -> CausalGrad:
+    """Gradients of dconv_causal(x, filt, bias, ...) from dout, the gradient of its output, and dstate_out, that of state_out.
+
+    dx may be given (a slice of a wider gradient, say); it is 0 behind `lengths`.  dstate is None without a state."""
+    dtype, index = _first(x, 3, "x")
+    N, L, C = x.shape
+    F = _taps(filt, C)
+    rows = (N, F - 1, C)
+    if dx is None:
+        dx = torch.empty((N, L, C), dtype=dtype, device=x.device)
+    sums = torch.empty(C * (F + 1), dtype=torch.float32, device=x.device)
+    dfilt, dbias = sums[:C * F].view(C, F), sums[C * F:]
+    dstate = None if state is None else torch.empty(rows, dtype=dtype, device=x.device)
+    fn = _lib()
+    head = (_DTYPES[dtype], N, L, C, F, 0, bool(silu), 0,
+            *_rows(x, (N, L, C), dtype, index, "x"), *_NONE, *_rows(dout, (N, L, C), dtype, index, "dout"),
+            *_rows(dx, (N, L, C), dtype, index, "dx", True),
+            _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
+            _dense(state, rows, dtype, index, "state"), 0, _dense(dstate_out, rows, dtype, index, "dstate_out"),
+            0 if dstate is None else dstate.data_ptr(), dfilt.data_ptr(), dbias.data_ptr(),
+            _dense(lengths, (N,), torch.int32, index, "lengths"), 0)
+    need = fn.dconv_causal_workspace(_CAUSAL.pack(*head, 0, 0))
+    ws = _workspace(need, index)
+    _run(fn.dconv_causal_grad, index, _CAUSAL.pack(*head, ws.data_ptr(), need))
+    return CausalGrad(dx, dfilt, dbias, dstate)
+
+
+def dconv_causal_step(x: torch.Tensor, state: torch.Tensor, filt: torch.Tensor, bias: torch.Tensor | None = None, *,
+                      silu: bool = True, slots: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """One token x [N,C] of each row: out [N,C], and the windows of `state` [M,F-1,C] move on by it.
+
+    slots [N] int32: the window of each row (default: row n has window n); rows with a slot outside the cache, or
+    one that an earlier row has, are padding: out is 0 there and no window changes."""
+    dtype, index = _first(x, 2, "x")
+    N, C = x.shape
+    F = _taps(filt, C)
+    if out is None:
+        out = torch.empty((N, C), dtype=dtype, device=x.device)
+    cache, M = _cache(state, (F - 1, C), dtype, index, "state", N, slots)
+    args = _CAUSAL.pack(
+        _DTYPES[dtype], N, 1, C, F, M, bool(silu), 0,
+        *_rows(x, (N, C), dtype, index, "x"), *_rows(out, (N, C), dtype, index, "out", True), *_NONE, *_NONE,
+        _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"), 0, cache, 0, 0, 0, 0,
+        0, _dense(slots, (N,), torch.int32, index, "slots"), 0, 0)
+    _run(_lib().dconv_causal_step, index, args)
+    return out
+
+
+def _taps(filt, C):
+    if not isinstance(filt, torch.Tensor) or filt.dim() != 2 or filt.shape[0] != C:
+        raise ValueError(f"filt must have the shape ({C}, F)")
+    return filt.shape[1]
+
+
+def _scan_sizes(u, A, B, dims):
+    dtype, index = _first(u, dims, "u")
+    if not isinstance(A, torch.Tensor) or A.dim() != 2 or A.shape[0] != u.shape[-1]:
+        raise ValueError("A must have the shape (C, S)")
+    if not isinstance(B, torch.Tensor) or B.dim() != dims + 1:
+        raise ValueError(f"B must have {dims + 1} dims")
+    return dtype, index, A.shape[1], B.shape[-2]
+
+
+def _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index):
+    """What all forms read: the token tensors, and the parameters."""
+    ch, S = A.shape
+    tokens = (_rows(u, wide, dtype, index, "u"), _rows(delta, wide, dtype, index, "delta"), _rows(z, wide, dtype, index, "z"))
+    bc = (_rows(B, narrow, dtype, index, "B"), _rows(C, narrow, dtype, index, "C"))
+    params = (_dense(A, (ch, S), torch.float32, index, "A"), _dense(D, (ch,), torch.float32, index, "D"),
+              _dense(delta_bias, (ch,), torch.float32, index, "delta_bias"))
+    return tokens, bc, params
+
+
+def scan_starts(N: int, L: int, C: int, S: int, G: int = 1, device="cuda") -> torch.Tensor:
+    """An empty tensor for the `starts` of dconv_scan and dconv_scan_grad on sequences of these sizes."""
+    need = _lib().dconv_scan_starts(_SCAN.pack(DTYPE_F32, N, L, C, S, G, 0, 0, *(12 * _NONE), *(15 * (0,))))
+    if need < 0:
+        from . import STATUS_BAD_SHAPE, _raise
+        _raise(STATUS_BAD_SHAPE)
+    return torch.empty(need // 4, dtype=torch.float32, device=device)
+
+
+def _starts(starts, N, L, C, S, G, index):
+    if starts is None:
+        return 0
+    need = _lib().dconv_scan_starts(_SCAN.pack(DTYPE_F32, N, L, C, S, G, 0, 0, *(12 * _NONE), *(15 * (0,))))
+    return _dense(starts, (max(need, 0) // 4,), torch.float32, index, "starts")
+
+
+def dconv_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor | None,
+               D: torch.Tensor | None = None, z: torch.Tensor | None = None, delta_bias: torch.Tensor | None = None, *,
+               softplus: bool = True, state: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+               out: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+               starts: torch.Tensor | None = None) -> torch.Tensor:
+    """The selective scan: with d = softplus(delta + delta_bias) (without softplus: delta + delta_bias),
+    h[t] = exp(d[t] A) h[t-1] + d[t] u[t] B[t],  y[t] = sum_s C[t] h[t] + D u[t],  out = y silu(z) or y.
+
+    u, delta, z [N,L,C]; B, C [N,L,G,S], group g for channels g*C/G onwards; one type for all of these.  A [C,S] (S <= 32),
+    D and delta_bias [C], fp32.  state [N,C,S] fp32: h before token 0 (default: zeros); state_out, which may be `state`,
+    receives h behind the last token.  lengths [N] int32: the tokens that count; out is 0 behind them.
+    starts (of scan_starts): receives what lets dconv_scan_grad go back without running the scan again."""
+    dtype, index, S, G = _scan_sizes(u, A, B, 3)
+    N, L, ch = u.shape
+    wide, narrow = (N, L, ch), (N, L, G, S)
+    tokens, bc, params = _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index)
+    if out is None:
+        out = torch.empty(wide, dtype=dtype, device=u.device)
+    head = (_DTYPES[dtype], N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
+            *_rows(out, wide, dtype, index, "out", True), *bc[0], *bc[1], *(6 * _NONE), *params,
+            _dense(state, (N, ch, S), torch.float32, index, "state"),
+            _dense(state_out, (N, ch, S), torch.float32, index, "state_out"), 0, 0, 0, 0, 0,
+            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), torch.int32, index, "lengths"), 0)
+    fn = _lib()
+    need = fn.dconv_scan_workspace(_SCAN.pack(*head, 0, 0), 0)
+    ws = _workspace(need, index)
+    _run(fn.dconv_scan, index, _SCAN.pack(*head, ws.data_ptr(), need))
+    return out
+
+
+def dconv_scan_grad(dout: torch.Tensor, u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                    C: torch.Tensor, D: torch.Tensor | None = None, z: torch.Tensor | None = None,
+                    delta_bias: torch.Tensor | None = None, *, softplus: bool = True, state: torch.Tensor | None = None,
+                    lengths: torch.Tensor | None = None, starts: torch.Tensor | None = None,
+                    dstate_out: torch.Tensor | None = None, du: torch.Tensor | None = None,
+                    ddelta: torch.Tensor | None = None, dz: torch.Tensor | None = None) -> ScanGrad:
+    """Gradients of dconv_scan(u, ...) from dout, the gradient of its output, and dstate_out, that of state_out.
+
+    starts: what dconv_scan left there for the same inputs; without it the states are made again.  du, ddelta and dz may be
+    given (slices of a wider gradient, say); gradients are 0 behind `lengths`."""
+    dtype, index, S, G = _scan_sizes(u, A, B, 3)
+    N, L, ch = u.shape
+    wide, narrow = (N, L, ch), (N, L, G, S)
+    tokens, bc, params = _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index)
+    make = lambda shape, t=dtype: torch.empty(shape, dtype=t, device=u.device)
+    du = make(wide) if du is None else du
+    ddelta = make(wide) if ddelta is None else ddelta
+    if z is None:
+        dz = None
+    elif dz is None:
+        dz = make(wide)
+    dB, dC, dA = make(narrow), make(narrow), make((ch, S), torch.float32)
+    dD = None if D is None else make((ch,), torch.float32)
+    dbias = None if delta_bias is None else make((ch,), torch.float32)
+    dstate = None if state is None else make((N, ch, S), torch.float32)
+    ptr = lambda t: 0 if t is None else t.data_ptr()
+    head = (_DTYPES[dtype], N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2], *_NONE, *bc[0], *bc[1],
+            *_rows(dout, wide, dtype, index, "dout"), *_rows(du, wide, dtype, index, "du", True),
+            *_rows(ddelta, wide, dtype, index, "ddelta", True), *_rows(dz, wide, dtype, index, "dz", True),
+            *_rows(dB, narrow, dtype, index, "dB"), *_rows(dC, narrow, dtype, index, "dC"), *params,
+            _dense(state, (N, ch, S), torch.float32, index, "state"), 0,
+            _dense(dstate_out, (N, ch, S), torch.float32, index, "dstate_out"), ptr(dstate), ptr(dA), ptr(dD), ptr(dbias),
+            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), torch.int32, index, "lengths"), 0)
+    fn = _lib()
+    need = fn.dconv_scan_workspace(_SCAN.pack(*head, 0, 0), 1)
+    ws = _workspace(need, index)
+    _run(fn.dconv_scan_grad, index, _SCAN.pack(*head, ws.data_ptr(), need))
+    return ScanGrad(du, ddelta, dA, dB, dC, dD, dz, dbias, dstate)
+
+
+def dconv_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor,
+                    state: torch.Tensor, D: torch.Tensor | None = None, z: torch.Tensor | None = None,
+                    delta_bias: torch.Tensor | None = None, *, softplus: bool = True, slots: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None) -> torch.Tensor:
+    """One token of each row: u, delta, z [N,C], B, C [N,G,S]; out [N,C], and `state` [M,C,S] (fp32) is updated.
+
+    slots as for dconv_causal_step."""
+    dtype, index, S, G = _scan_sizes(u, A, B, 2)
+    N, ch = u.shape
+    wide, narrow = (N, ch), (N, G, S)
+    if out is None:
+        out = torch.empty(wide, dtype=dtype, device=u.device)
+    tokens = [_rows(t, wide, dtype, index, what) for t, what in ((u, "u"), (delta, "delta"), (z, "z"))]
+    bc = []
+    for t, what in ((B, "B"), (C, "C")):                       # [N, G, S]: the middle stride is the groups'
+        p, sn, sg, _ = _rows(t, narrow, dtype, index, what)
+        bc.append((p, sn, 0, sg))
+    cache, M = _cache(state, (ch, S), torch.float32, index, "state", N, slots)
+    args = _SCAN.pack(
+        _DTYPES[dtype], N, 1, ch, S, G, M, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
+        *_rows(out, wide, dtype, index, "out", True), *bc[0], *bc[1], *(6 * _NONE),
+        _dense(A, (ch, S), torch.float32, index, "A"), _dense(D, (ch,), torch.float32, index, "D"),
+        _dense(delta_bias, (ch,), torch.float32, index, "delta_bias"), 0, cache, 0, 0, 0, 0, 0, 0, 0,
+        _dense(slots, (N,), torch.int32, index, "slots"), 0, 0)
+    _run(_lib().dconv_scan_step, index, args)
+    return out
