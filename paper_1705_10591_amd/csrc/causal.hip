@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kAhead = 8;            // rows of a strip that are read together; strips are multiples of it, so that
                                      // only the first one reaches into the state (F - 1 <= 7 rows)
+constexpr int kGradAhead = 4;
 
 struct CausalParams {
     const void *x, *filt, *bias, *state, *dout, *dstate_out;
@@ -53,8 +54,7 @@ __device__ __forceinline__ void load_filter(const T* filt, int c, int nv, float 
     float flat[F * V];
 #pragma unroll
     for (int q = 0; q < F; ++q) {
-        float part[V];
-        load_some<V>(filt + (int64_t)c * F + q * V, nv * F - q * V, part);
+        const Run<T, V> part = load_some<V>(filt + (int64_t)c * F + q * V, nv * F - q * V);
 #pragma unroll
         for (int i = 0; i < V; ++i) flat[q * V + i] = part[i];
     }
@@ -75,20 +75,28 @@ causal_kernel(CausalParams p)
     T* out = (T*)p.out + a.n * p.o_n + a.c;
     const int64_t first = (int64_t)a.n * (F - 1) * p.C + a.c;
 
-    float w[F][V], bias[V] = {}, rows[kAhead + F - 1][V];
-    load_filter<T, F, V>((const T*)p.filt, a.c, a.nv, w);
-    if (p.bias) load_some<V>((const T*)p.bias + a.c, a.nv, bias);
+    // rows are loaded together and without conditions: one that does not count reads the last one that does, and what is
+    // made of it is not written
+    Run<T, V> in[kAhead], before[F];
+    auto fetch = [&](int t0) {
+        if (len == 0) return;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) in[k] = load_some<V>(x + min(t0 + k, len - 1) * p.x_l, a.nv);
+    };
 #pragma unroll
     for (int r = 0; r < F - 1; ++r) {
         const int t = a.t0 - (F - 1) + r;
+        before[r] = Run<T, V>{};
         if (t >= 0) {
-            if (t < len) load_some<V>(x + t * p.x_l, a.nv, rows[r]);
+            if (len) before[r] = load_some<V>(x + min(t, len - 1) * p.x_l, a.nv);
         } else if (p.state) {
-            load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv, rows[r]);
-        } else {
-            for (int i = 0; i < V; ++i) rows[r][i] = 0.f;
+            before[r] = load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv);
         }
     }
+    fetch(a.t0);
+    float w[F][V], bias[V] = {}, rows[kAhead + F - 1][V];
+    load_filter<T, F, V>((const T*)p.filt, a.c, a.nv, w);
+    if (p.bias) load_some<V>((const T*)p.bias + a.c, a.nv, bias);
     // the last F-1 rows of the sequence, by the thread that has read the state's (which they may overwrite)
     if (a.t0 == 0 && p.state_out) {
         for (int r = 0; r < F - 1; ++r) {
@@ -99,10 +107,16 @@ causal_kernel(CausalParams p)
             store_some<V>((T*)p.state_out + first + (int64_t)r * p.C, a.nv, v);
         }
     }
+#pragma unroll
+    for (int r = 0; r < F - 1; ++r)
+#pragma unroll
+        for (int i = 0; i < V; ++i) rows[r][i] = before[r][i];
     for (int t0 = a.t0; t0 < end; t0 += kAhead) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (t0 + k < min(end, len)) load_some<V>(x + (t0 + k) * p.x_l, a.nv, rows[F - 1 + k]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) rows[F - 1 + k][i] = in[k][i];
+        if (t0 + kAhead < end) fetch(t0 + kAhead);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             float y[V];
@@ -140,39 +154,53 @@ causal_grad_kernel(CausalParams p)
         const T* dout = (const T*)p.dout + a.n * p.g_n + a.c;
         T* dx = (T*)p.dx + a.n * p.d_n + a.c;
         const int64_t first = (int64_t)a.n * (F - 1) * p.C + a.c;
+        const int stop = (int)min((int64_t)end + F - 1, (int64_t)kMaxTokens + 16);
+        Run<T, V> xn[kGradAhead], gn[kGradAhead], before[F];
+        auto fetch = [&](int t0) {                   // (as in causal_kernel)
+            if (len == 0) return;
+#pragma unroll
+            for (int k = 0; k < kGradAhead; ++k) {
+                xn[k] = load_some<V>(x + min(t0 + k, len - 1) * p.x_l, a.nv);
+                gn[k] = load_some<V>(dout + min(t0 + k, len - 1) * p.g_l, a.nv);
+            }
+        };
+#pragma unroll
+        for (int r = 0; r < F - 1; ++r) {
+            const int t = a.t0 - (F - 1) + r;
+            before[r] = Run<T, V>{};
+            if (t >= 0) {
+                if (len) before[r] = load_some<V>(x + min(t, len - 1) * p.x_l, a.nv);
+            } else if (p.state) {
+                before[r] = load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kGradAhead; ++k) xn[k] = gn[k] = Run<T, V>{};
+        fetch(a.t0);
         float w[F][V], bias[V] = {}, rows[F][V], ds[F][V] = {};
         load_filter<T, F, V>((const T*)p.filt, a.c, a.nv, w);
         if (p.bias) load_some<V>((const T*)p.bias + a.c, a.nv, bias);
 #pragma unroll
-        for (int r = 0; r < F - 1; ++r) {            // rows[1 ..]: they move down by one before each token
-            const int t = a.t0 - (F - 1) + r;
-            for (int i = 0; i < V; ++i) rows[r + 1][i] = 0.f;
-            if (t >= 0) {
-                if (t < len) load_some<V>(x + t * p.x_l, a.nv, rows[r + 1]);
-            } else if (p.state) {
-                load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv, rows[r + 1]);
-            }
-        }
-        const int64_t stop = (int64_t)end + F - 1;
-        for (int64_t t0 = a.t0; t0 < stop; t0 += 4) {
-            float xn[4][V], gn[4][V];
+        for (int r = 0; r < F - 1; ++r)              // rows[1 ..]: they move down by one before each token
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                for (int i = 0; i < V; ++i) xn[k][i] = gn[k][i] = 0.f;
-                if (t0 + k < min(stop, (int64_t)len)) {
-                    load_some<V>(x + (t0 + k) * p.x_l, a.nv, xn[k]);
-                    load_some<V>(dout + (t0 + k) * p.g_l, a.nv, gn[k]);
-                }
-            }
+            for (int i = 0; i < V; ++i) rows[r + 1][i] = before[r][i];
+        for (int t0 = a.t0; t0 < stop; t0 += kGradAhead) {
+            Run<T, V> xc[kGradAhead], gc[kGradAhead];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int64_t t = t0 + k;
+            for (int k = 0; k < kGradAhead; ++k) {
+                xc[k] = xn[k];
+                gc[k] = gn[k];
+            }
+            if (t0 + kGradAhead < stop) fetch(t0 + kGradAhead);
+#pragma unroll
+            for (int k = 0; k < kGradAhead; ++k) {
+                const int t = t0 + k;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
 #pragma unroll
                     for (int j = 0; j < F - 1; ++j) { rows[j][i] = rows[j + 1][i]; ds[j][i] = ds[j + 1][i]; }
-                    rows[F - 1][i] = xn[k][i];
-                    float s = bias[i], d = gn[k][i];
+                    rows[F - 1][i] = xc[k][i];
+                    float s = bias[i], d = gc[k][i];
 #pragma unroll
                     for (int j = 0; j < F; ++j) s = __builtin_fmaf(w[j][i], rows[j][i], s);
                     if (p.silu) {
@@ -188,7 +216,7 @@ causal_grad_kernel(CausalParams p)
                     }
                 }
                 // the row that has all of its terms now; before token 0 it is one of the state
-                const int64_t r = t - (F - 1);
+                const int r = t - (F - 1);
                 if (r < end && (r >= a.t0 || (a.t0 == 0 && p.dstate))) {
                     float v[V];
 #pragma unroll
@@ -197,14 +225,14 @@ causal_grad_kernel(CausalParams p)
 #pragma unroll
                         for (int j = 0; j < F; ++j) v[i] = __builtin_fmaf(w[j][i], ds[F - 1 - j][i], v[i]);
                     }
-                    const int64_t i = r - len + F - 1;           // of state_out, if it went there
+                    const int i = r - len + F - 1;               // of state_out, if it went there
                     if (p.dstate_out && i >= 0 && i < F - 1) {
                         float e[V];
-                        load_some<V>((const T*)p.dstate_out + first + i * p.C, a.nv, e);
+                        load_some<V>((const T*)p.dstate_out + first + (int64_t)i * p.C, a.nv, e);
                         for (int k2 = 0; k2 < V; ++k2) v[k2] += e[k2];
                     }
                     if (r >= 0) store_some<V>(dx + r * p.d_l, a.nv, v);
-                    else store_some<V>((T*)p.dstate + first + (F - 1 + r) * p.C, a.nv, v);
+                    else store_some<V>((T*)p.dstate + first + (int64_t)(F - 1 + r) * p.C, a.nv, v);
                 }
             }
         }

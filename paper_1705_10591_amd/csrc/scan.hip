@@ -5,17 +5,16 @@ namespace dconv {
 
 namespace {
 
-// B and C of a token and wave, side by side in fp32.
+// B and C of a token and wave, side by side in fp32: thread i has the i-th eight of the layout.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 bc_kernel(Rows B, Rows C, int64_t b_g, int64_t c_g, const int* lengths, float* bc, int N, int L, int G, int S, int W,
-          int tokens)
+          int tiles)
 {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t row = i / W;
-    const int s0 = (int)(i - row * W) * kR;
-    const int64_t seq = row / tokens;
-    const int t = (int)(row - seq * tokens), n = (int)(seq / G), g = (int)(seq - (int64_t)n * G);
+    const int64_t unit = i / kT, tile = unit / W, seq = tile / tiles;
+    const int s0 = (int)(unit - tile * W) * kR;
+    const int t = (int)(tile - seq * tiles) * kT + (int)(i - unit * kT), n = (int)(seq / G), g = (int)(seq - (int64_t)n * G);
     if (n >= N) return;
     float b[kR] = {}, c[kR] = {};
     if (t < length_of(lengths, n, L)) {
@@ -67,51 +66,65 @@ scan_kernel(ScanParams p, bool ends)
         }
     }
 
-    float dbias[E] = {}, skip[E] = {}, u[E] = {}, dl[E] = {}, z[E] = {};
+    float dbias[E] = {}, skip[E] = {};
     if (nv > 0) {
         if (p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
         if (OUT && p.D) load_some<E>(p.D + ec, nv, skip);
     }
     const bool gate = OUT && p.z.p;
-    auto fetch = [&](int tile) {
-        const int t = tile * kT + tt;
-        if (tile < a.stop && t < a.len && nv > 0) {
-            load_some<E>(p.u.at<const T>(a.n, t, ec), nv, u);
-            load_some<E>(p.delta.at<const T>(a.n, t, ec), nv, dl);
-            if (gate) load_some<E>(p.z.at<const T>(a.n, t, ec), nv, z);
-        }
+    Run<T, E> u{}, dl{}, z{};
+    auto fetch = [&](int tile) {                          // (a token that does not count reads the last that does)
+        if (tile >= a.stop || nv <= 0) return;
+        const int t = min(tile * kT + tt, a.len - 1);
+        u = load_some<E>(p.u.at<const T>(a.n, t, ec), nv);
+        dl = load_some<E>(p.delta.at<const T>(a.n, t, ec), nv);
+        if (gate) z = load_some<E>(p.z.at<const T>(a.n, t, ec), nv);
     };
-    bc_ptr bc = bc_of(p, a, W, wave) + (int64_t)a.tile0 * kT * W;
     fetch(a.tile0);
-    for (int tile = a.tile0; tile < a.stop; ++tile, bc += kT * W) {
+    BC bc, next;
+    if (a.tile0 < a.stop) bc.load(bc_of(p, a, a.tile0, W, wave));
+    for (int tile = a.tile0; tile < a.stop; ++tile) {
         const int t = tile * kT + tt;
-        float uc[E], zc[E];
+        const bool in = t < a.len;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             const float raw = dl[i] + dbias[i];
-            const bool in = t < a.len && i < nv;
-            const float d = in ? (p.softplus ? softplus(raw) : raw) : 0.f;
-            uc[i] = u[i];
-            zc[i] = z[i];
-            step[tt][tc + i] = make_float2(d, in ? d * u[i] : 0.f);
+            const float d = in && i < nv ? (p.softplus ? softplus(raw) : raw) : 0.f;
+            step[tt][tc + i] = make_float2(d, in && i < nv ? d * u[i] : 0.f);
         }
+        const Run<T, E> uc = u, zc = z;
         fetch(tile + 1);
-        __syncthreads();
+        meet();
         if (p.starts && !ends) store_states(p.starts + lane_states(p, a, (int64_t)a.n * p.tiles + tile, W, wave, lane), h);
+        float2 d[kStep], dn[kStep];
 #pragma unroll
-        for (int k = 0; k < kT; ++k) {
-            const float2 d = step[k][lane];
-            const f8 v = bc[k * W];
-            float y = 0.f;
+        for (int k = 0; k < kStep; ++k) d[k] = step[k][lane];
+        const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, min(tile + 1, a.stop - 1), W, wave);
 #pragma unroll
-            for (int r = 0; r < kR; ++r) {
-                h[r] = __builtin_fmaf(exp2_(d.x * A[r]), h[r], d.y * v[r]);
-                if (OUT) y = r ? __builtin_fmaf(v[kR + r], h[r], y) : v[kR + r] * h[r];
+        for (int k0 = 0; k0 < kT; k0 += kStep) {
+            const bool more = k0 + kStep < kT;
+            next.load(more ? here + (k0 + kStep) / 2 : after);
+#pragma unroll
+            for (int k = 0; k < kStep; ++k)
+                if (more) dn[k] = step[k0 + kStep + k][lane];
+            in_order();
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) {
+                float y = 0.f;
+#pragma unroll
+                for (int r = 0; r < kR; ++r) {
+                    h[r] = __builtin_fmaf(exp2_(d[k].x * A[r]), h[r], d[k].y * bc.b(k, r));
+                    if (OUT) y = r ? __builtin_fmaf(bc.c(k, r), h[r], y) : bc.c(k, r) * h[r];
+                }
+                if (OUT) ysum[wave][k0 + k][lane] = y;
+                else dtotal += d[k].x;
             }
-            if (OUT) ysum[wave][k][lane] = y;
-            else dtotal += d.x;
+            in_order();
+            bc = next;
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) d[k] = dn[k];
         }
-        __syncthreads();
+        meet();
         if (OUT && nv > 0 && t < p.L) {
             float y[E];
 #pragma unroll
@@ -120,7 +133,7 @@ scan_kernel(ScanParams p, bool ends)
 #pragma unroll
                 for (int w = 0; w < W; ++w) y[i] += ysum[w][tt][tc + i];
                 if (gate) y[i] *= zc[i] * sigmoid(zc[i]);
-                if (t >= a.len) y[i] = 0.f;
+                if (!in) y[i] = 0.f;
             }
             store_some<E>(p.out.at<T>(a.n, t, ec), nv, y);
         }
@@ -240,13 +253,12 @@ ScanParams scan_params(const dconv_scan_args& a, const ScanPlan& pl)
 
 int launch_scan_bc(const dconv_scan_args& a, const ScanPlan& pl, float* bc, hipStream_t st)
 {
-    const int tokens = pl.tiles * kT;
-    const int64_t n = (int64_t)a.N * a.G * tokens * pl.waves;
+    const int64_t n = (int64_t)a.N * a.G * pl.tiles * kT * pl.waves;
     const dim3 grid((unsigned)((n + kThreads - 1) / kThreads));
     begin_launch();
     auto go = [&](auto* kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, rows_of(a.B), rows_of(a.Cm), a.B.sg, a.Cm.sg, a.lengths, bc,
-                           a.N, a.L, a.G, a.S, pl.waves, tokens);
+                           a.N, a.L, a.G, a.S, pl.waves, pl.tiles);
     };
     if (a.dtype == DCONV_DTYPE_F16) go(&bc_kernel<_Float16>);
     else if (a.dtype == DCONV_DTYPE_BF16) go(&bc_kernel<__bf16>);

@@ -68,35 +68,52 @@ scan_back_kernel(ScanParams p)
     if (a.chunk == p.chunks - 1 && p.dstate_out)
         load_states(p.dstate_out + ((int64_t)a.n * p.C + c) * p.S, s0, p.S, lane < a.nc, carry);
     if (nv > 0 && p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
+    Run<T, E> dl{}, go{}, z{};
+    auto fetch = [&](int tile) {
+        if (tile < a.tile0 || nv <= 0) return;
+        const int t = min(tile * kT + tt, a.len - 1);
+        dl = load_some<E>(p.delta.at<const T>(a.n, t, ec), nv);
+        go = load_some<E>(p.dout.at<const T>(a.n, t, ec), nv);
+        if (p.z.p) z = load_some<E>(p.z.at<const T>(a.n, t, ec), nv);
+    };
+    BC bc, next;
+    if (a.stop > a.tile0) {
+        fetch(a.stop - 1);
+        bc.load(bc_of(p, a, a.stop - 1, W, wave) + (kT - kStep) / 2);
+    }
     for (int tile = a.stop - 1; tile >= a.tile0; --tile) {
-        const int t = tile * kT + tt;
-        const bool in = t < a.len && nv > 0;
-        float dl[E] = {}, dy[E] = {}, z[E];
-        if (in) {
-            load_some<E>(p.delta.at<const T>(a.n, t, ec), nv, dl);
-            load_some<E>(p.dout.at<const T>(a.n, t, ec), nv, dy);
-            if (p.z.p) {
-                load_some<E>(p.z.at<const T>(a.n, t, ec), nv, z);
-#pragma unroll
-                for (int i = 0; i < E; ++i) dy[i] *= z[i] * sigmoid(z[i]);
-            }
-        }
-        __syncthreads();
+        const bool in = tile * kT + tt < a.len;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             const float raw = dl[i] + dbias[i];
-            step[tt][tc + i] = make_float2(in && i < nv ? (p.softplus ? softplus(raw) : raw) : 0.f, in && i < nv ? dy[i] : 0.f);
+            const float d = p.softplus ? softplus(raw) : raw, dy = p.z.p ? go[i] * z[i] * sigmoid(z[i]) : go[i];
+            step[tt][tc + i] = in && i < nv ? make_float2(d, dy) : make_float2(0.f, 0.f);
         }
-        __syncthreads();
-        bc_ptr bc = bc_of(p, a, W, wave) + (int64_t)tile * kT * W;
+        fetch(tile - 1);
+        meet();
+        float2 d[kStep], dn[kStep];
 #pragma unroll
-        for (int k = kT - 1; k >= 0; --k) {
-            const float2 d = step[k][lane];
-            const f8 v = bc[k * W];
+        for (int k = 0; k < kStep; ++k) d[k] = step[kT - kStep + k][lane];
+        const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, max(tile - 1, a.tile0), W, wave);
 #pragma unroll
-            for (int r = 0; r < kR; ++r) carry[r] = exp2_(d.x * A[r]) * __builtin_fmaf(v[kR + r], d.y, carry[r]);
-            dtotal += d.x;
+        for (int k0 = kT - kStep; k0 >= 0; k0 -= kStep) {
+            next.load(k0 ? here + (k0 - kStep) / 2 : after + (kT - kStep) / 2);
+#pragma unroll
+            for (int k = 0; k < kStep; ++k)
+                if (k0) dn[k] = step[k0 - kStep + k][lane];
+            in_order();
+#pragma unroll
+            for (int k = kStep - 1; k >= 0; --k) {
+#pragma unroll
+                for (int r = 0; r < kR; ++r) carry[r] = exp2_(d[k].x * A[r]) * __builtin_fmaf(bc.c(k, r), d[k].y, carry[r]);
+                dtotal += d[k].x;
+            }
+            in_order();
+            bc = next;
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) d[k] = dn[k];
         }
+        meet();
     }
     const int64_t row = (int64_t)a.n * p.chunks + a.chunk;
     store_states(p.back + lane_states(p, a, row, W, wave, lane), carry);
@@ -144,72 +161,121 @@ scan_grad_kernel(ScanParams p)
             if (gate) store_some<E>(p.dz.at<T>(a.n, t, ec), nv, zero);
         }
     }
+    // what a tile reads, asked for a tile ahead
+    Run<T, E> un{}, dln{}, gon{}, zn{};
+    float hn[kR] = {};
+    auto fetch = [&](int tile) {
+        if (tile < a.tile0) return;
+        load_states(p.starts + lane_states(p, a, (int64_t)a.n * p.tiles + tile, W, wave, lane), hn);
+        if (nv <= 0) return;
+        const int t = min(tile * kT + tt, a.len - 1);
+        un = load_some<E>(p.u.at<const T>(a.n, t, ec), nv);
+        dln = load_some<E>(p.delta.at<const T>(a.n, t, ec), nv);
+        gon = load_some<E>(p.dout.at<const T>(a.n, t, ec), nv);
+        if (gate) zn = load_some<E>(p.z.at<const T>(a.n, t, ec), nv);
+    };
+    BC bc, next;
+    if (a.stop > a.tile0) {
+        fetch(a.stop - 1);
+        bc.load(bc_of(p, a, a.stop - 1, W, wave));
+    }
     for (int tile = a.stop - 1; tile >= a.tile0; --tile) {
         const int t = tile * kT + tt;
         const bool in = t < a.len && nv > 0;
-        float u[E] = {}, dl[E] = {}, go[E] = {}, z[E] = {}, d[E];
-        if (in) {
-            load_some<E>(p.u.at<const T>(a.n, t, ec), nv, u);
-            load_some<E>(p.delta.at<const T>(a.n, t, ec), nv, dl);
-            load_some<E>(p.dout.at<const T>(a.n, t, ec), nv, go);
-            if (gate) load_some<E>(p.z.at<const T>(a.n, t, ec), nv, z);
-        }
+        Run<T, E> u = un, dl = dln, go = gon, z = zn;
         float h0[kR];
-        load_states(p.starts + lane_states(p, a, (int64_t)a.n * p.tiles + tile, W, wave, lane), h0);
+#pragma unroll
+        for (int r = 0; r < kR; ++r) h0[r] = hn[r];
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             const float raw = dl[i] + dbias[i];
-            d[i] = in && i < nv ? (p.softplus ? softplus(raw) : raw) : 0.f;
-            step[tt][tc + i] = make_float2(d[i], d[i] * u[i]);
-            gout[tt][tc + i] = gate ? go[i] * z[i] * sigmoid(z[i]) : go[i];
+            const float d = p.softplus ? softplus(raw) : raw;
+            const bool on = in && i < nv;
+            step[tt][tc + i] = on ? make_float2(d, d * u[i]) : make_float2(0.f, 0.f);
+            gout[tt][tc + i] = !on ? 0.f : gate ? go[i] * z[i] * sigmoid(z[i]) : go[i];
         }
-        __syncthreads();
-        bc_ptr bc = bc_of(p, a, W, wave) + (int64_t)tile * kT * W;
+        fetch(tile - 1);
+        meet();
+        const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, max(tile - 1, a.tile0), W, wave);
         float dec[kT][kR], h[kT][kR];
+        float2 s[kStep], sn[kStep];
 #pragma unroll
-        for (int k = 0; k < kT; ++k) {
-            const float2 s = step[k][lane];
-            const f8 v = bc[k * W];
-            float y = 0.f;
+        for (int k = 0; k < kStep; ++k) s[k] = step[k][lane];
 #pragma unroll
-            for (int r = 0; r < kR; ++r) {
-                dec[k][r] = exp2_(s.x * (A[r] * kLog2e));
-                h[k][r] = __builtin_fmaf(dec[k][r], k ? h[k - 1][r] : h0[r], s.y * v[r]);
-                y = r ? __builtin_fmaf(v[kR + r], h[k][r], y) : v[kR + r] * h[k][r];
+        for (int k0 = 0; k0 < kT; k0 += kStep) {
+            const bool more = k0 + kStep < kT;
+            if (more) next.load(here + (k0 + kStep) / 2);
+#pragma unroll
+            for (int k = 0; k < kStep; ++k)
+                if (more) sn[k] = step[k0 + kStep + k][lane];
+            in_order();
+#pragma unroll
+            for (int k = k0; k < k0 + kStep; ++k) {
+                float y = 0.f;
+#pragma unroll
+                for (int r = 0; r < kR; ++r) {
+                    dec[k][r] = exp2_(s[k - k0].x * (A[r] * kLog2e));
+                    h[k][r] = __builtin_fmaf(dec[k][r], k ? h[k - 1][r] : h0[r], s[k - k0].y * bc.b(k - k0, r));
+                    y = r ? __builtin_fmaf(bc.c(k - k0, r), h[k][r], y) : bc.c(k - k0, r) * h[k][r];
+                }
+                if (gate) sums[0][wave][k][lane] = y;
             }
-            if (gate) sums[0][wave][k][lane] = y;
-        }
-        float packed[8];
+            in_order();
+            if (more) {
+                bc = next;
 #pragma unroll
-        for (int k = kT - 1; k >= 0; --k) {
-            const float2 s = step[k][lane];
-            const float dy = gout[k][lane];
-            const f8 v = bc[k * W];
-            float q = 0.f, ea = 0.f, pair[kR];
-#pragma unroll
-            for (int r = 0; r < kR; ++r) {
-                const float g = __builtin_fmaf(v[kR + r], dy, carry[r]);
-                carry[r] = g * dec[k][r];
-                const float e = carry[r] * (k ? h[k - 1][r] : h0[r]);
-                q = r ? __builtin_fmaf(g, v[r], q) : g * v[r];
-                ea = r ? __builtin_fmaf(e, A[r], ea) : e * A[r];
-                dA[r] = __builtin_fmaf(e, s.x, dA[r]);
-                pair[r] = fold32(g * s.y, dy * h[k][r]);
-            }
-            sums[1][wave][k][lane] = q;
-            sums[2][wave][k][lane] = ea;
-            packed[k & 7] = fold<kAcross8>(fold16(pair[0], pair[2]), fold16(pair[1], pair[3]), lane & 8);
-            if ((k & 7) == 0) {
-                float f[4], e[2];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) f[i] = fold<kAcross4>(packed[i], packed[i + 4], lane & 4);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) e[i] = fold<kAcross2>(f[i], f[i + 2], lane & 2);
-                const int64_t at = (((int64_t)a.block * p.N + a.n) * p.tiles + tile) * 2 + k / 8;
-                p.part_bc[(at * W + wave) * kWave + lane] = fold<kAcross1>(e[0], e[1], lane & 1);
+                for (int k = 0; k < kStep; ++k) s[k] = sn[k];
             }
         }
-        __syncthreads();
+        float packed[8], dy[kStep], dyn[kStep];
+#pragma unroll
+        for (int k = 0; k < kStep; ++k) dy[k] = gout[kT - kStep + k][lane];
+#pragma unroll
+        for (int k0 = kT - kStep; k0 >= 0; k0 -= kStep) {
+            next.load(k0 ? here + (k0 - kStep) / 2 : after);
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) {
+                if (!k0) continue;
+                sn[k] = step[k0 - kStep + k][lane];
+                dyn[k] = gout[k0 - kStep + k][lane];
+            }
+            in_order();
+#pragma unroll
+            for (int k = k0 + kStep - 1; k >= k0; --k) {
+                const int j = k - k0;
+                float q = 0.f, ea = 0.f, pair[kR];
+#pragma unroll
+                for (int r = 0; r < kR; ++r) {
+                    const float g = __builtin_fmaf(bc.c(j, r), dy[j], carry[r]);
+                    carry[r] = g * dec[k][r];
+                    const float e = carry[r] * (k ? h[k - 1][r] : h0[r]);
+                    q = r ? __builtin_fmaf(g, bc.b(j, r), q) : g * bc.b(j, r);
+                    ea = r ? __builtin_fmaf(e, A[r], ea) : e * A[r];
+                    dA[r] = __builtin_fmaf(e, s[j].x, dA[r]);
+                    pair[r] = fold32(g * s[j].y, dy[j] * h[k][r]);
+                }
+                sums[1][wave][k][lane] = q;
+                sums[2][wave][k][lane] = ea;
+                packed[k & 7] = fold<kAcross8>(fold16(pair[0], pair[2]), fold16(pair[1], pair[3]), lane & 8);
+                if ((k & 7) == 0) {
+                    float f[4], e[2];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f[i] = fold<kAcross4>(packed[i], packed[i + 4], lane & 4);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) e[i] = fold<kAcross2>(f[i], f[i + 2], lane & 2);
+                    const int64_t at = (((int64_t)a.block * p.N + a.n) * p.tiles + tile) * 2 + k / 8;
+                    p.part_bc[(at * W + wave) * kWave + lane] = fold<kAcross1>(e[0], e[1], lane & 1);
+                }
+            }
+            in_order();
+            bc = next;
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) {
+                s[k] = sn[k];
+                dy[k] = dyn[k];
+            }
+        }
+        meet();
         if (nv > 0 && t < p.L) {
             float du[E], dd[E], dz[E];
 #pragma unroll
@@ -221,13 +287,13 @@ scan_grad_kernel(ScanParams p)
                     q += sums[1][w][tt][tc + i];
                     ea += sums[2][w][tt][tc + i];
                 }
-                const float sg = sigmoid(z[i]), dy = gate ? go[i] * z[i] * sg : go[i];
-                du[i] = __builtin_fmaf(d[i], q, skip[i] * dy);
+                const float sg = gate ? sigmoid(z[i]) : 0.f, dy = gate ? go[i] * z[i] * sg : go[i];
+                du[i] = __builtin_fmaf(step[tt][tc + i].x, q, skip[i] * dy);
                 dd[i] = __builtin_fmaf(u[i], q, ea);
                 if (p.softplus) dd[i] *= sigmoid(dl[i] + dbias[i]);
-                dz[i] = go[i] * y * (sg * (1.f + z[i] * (1.f - sg)));
+                dz[i] = gate ? go[i] * y * (sg * (1.f + z[i] * (1.f - sg))) : 0.f;
                 if (!in) du[i] = dd[i] = dz[i] = 0.f;
-                sumD[i] = __builtin_fmaf(dy, u[i], sumD[i]);
+                else sumD[i] = __builtin_fmaf(dy, u[i], sumD[i]);
                 sumB[i] += dd[i];
             }
             store_some<E>(p.du.at<T>(a.n, t, ec), nv, du);

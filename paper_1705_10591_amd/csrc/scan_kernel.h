@@ -7,9 +7,12 @@
 //    states of the same channels; what all states of a channel share (d, d u, the sum over states) goes through LDS.
 //  * Tokens come in tiles of kT = 16.  Thread by thread a tile's 16 x 64 values are loaded and stored in runs of E = 16 / W
 //    channels, and d, its softplus and the gate are computed once, not once per wave.
-//  * bc_kernel lays B and C out for the scalar loads first: fp32, [N][G][tokens][W][4 of B, 4 of C], zeros behind the end
-//    of a sequence and beyond state S.  With d = 0 there too, tokens that do not count leave the state as it is, and
-//    the loops need no masks.
+//  * bc_kernel lays B and C out for the scalar loads first: fp32, [N][G][tiles][W][16 tokens][4 of B, 4 of C], zeros behind
+//    the end of a sequence and beyond state S.  With d = 0 there too, tokens that do not count leave the state as it is,
+//    and the loops need no masks.
+//  * Scalar loads come back in any order, so that a wait for one is a wait for all: a tile is walked in steps of kStep = 4
+//    tokens, and the operands of the next step (64 of B and C in scalar registers, d and d u from LDS) are asked for before the
+//    arithmetic of this one.
 //  * A call with too few (sequence, channel block) pairs for the chip cuts its sequences into chunks: a first launch
 //    runs each chunk from a state of zero, and each workgroup of the second begins by putting together what the chunks
 //    before it leave, since a chunk changes the state it is given by the factor exp(A sum d) alone.
@@ -20,11 +23,24 @@ namespace dconv {
 
 constexpr int kT = 16;               // tokens of a tile
 constexpr int kR = 4;                // states of a wave
+constexpr int kStep = 4;             // tokens whose operands are fetched together
 constexpr int kMaxStates = 32;       // eight waves
 
 typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef float f8 __attribute__((ext_vector_type(8), aligned(16)));
-typedef const __attribute__((address_space(4))) f8* bc_ptr;        // constant memory: scalar loads
+typedef float f16 __attribute__((ext_vector_type(16), aligned(16)));
+typedef const __attribute__((address_space(4))) f16* bc_ptr;       // constant memory: scalar loads, two tokens each
+
+// B and C of kStep tokens.
+struct BC {
+    f16 v[kStep / 2];
+    __device__ __forceinline__ void load(bc_ptr p)
+    {
+#pragma unroll
+        for (int i = 0; i < kStep / 2; ++i) v[i] = p[i];
+    }
+    __device__ __forceinline__ float b(int k, int r) const { return v[k / 2][k % 2 * 8 + r]; }
+    __device__ __forceinline__ float c(int k, int r) const { return v[k / 2][k % 2 * 8 + kR + r]; }
+};
 
 struct Rows {                        // a token tensor: base, elements between sequences and tokens
     void* p;
@@ -75,10 +91,14 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanParams& p)
     return a;
 }
 
-__device__ __forceinline__ bc_ptr bc_of(const ScanParams& p, const ScanPlace& a, int W, int wave)
+// ... of a wave and tile; a token takes half an f16
+__device__ __forceinline__ bc_ptr bc_of(const ScanParams& p, const ScanPlace& a, int tile, int W, int wave)
 {
-    return (bc_ptr)(p.bc) + ((int64_t)a.n * p.G + a.g) * p.tiles * kT * W + wave;
+    return (bc_ptr)(p.bc) + ((((int64_t)a.n * p.G + a.g) * p.tiles + tile) * W + wave) * (kT / 2);
 }
+
+// Nothing moves past this point: what is written above it is under way before what is written below begins.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // Index of this lane's four states among those of all channels.
 __device__ __forceinline__ int64_t lane_states(const ScanParams& p, const ScanPlace& a, int64_t row, int W, int wave, int lane)

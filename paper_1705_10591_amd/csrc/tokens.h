@@ -4,46 +4,69 @@
 
 namespace dconv {
 
-template <int N> using vf = float __attribute__((ext_vector_type(N)));
-
-// N elements that lie next to each other, as fp32.  The hardware takes loads and stores of up to 16 bytes at any address
-// (an odd number of channels moves every other row off its alignment), so that there is one kernel for all alignments.
-template <int N, typename T> __device__ __forceinline__ void load_run(const T* p, float (&v)[N])
-{
+// N elements that lie next to each other.  The hardware takes loads and stores of up to 16 bytes at any address (an odd
+// number of channels moves every other row off its alignment), so that there is one kernel for all alignments.
+template <typename T, int N> struct Run {
     typedef T vt __attribute__((ext_vector_type(N)));
-    vt t;
-    __builtin_memcpy(&t, p, sizeof(T) * N);
-    for (int i = 0; i < N; ++i) v[i] = (float)t[i];
-}
-template <typename T> __device__ __forceinline__ void load_run(const T* p, float (&v)[1]) { v[0] = (float)p[0]; }
+    vt v;
+    __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
+};
+template <typename T> struct Run<T, 1> {
+    T v;
+    __device__ __forceinline__ float operator[](int) const { return (float)v; }
+};
 
-template <int N, typename T> __device__ __forceinline__ void store_run(T* p, const float (&v)[N])
+template <int N, typename T> __device__ __forceinline__ Run<T, N> load_run(const T* p)
 {
-    typedef T vt __attribute__((ext_vector_type(N)));
-    vt t;
-    for (int i = 0; i < N; ++i) t[i] = (T)v[i];           // round to nearest even
-    __builtin_memcpy(p, &t, sizeof(T) * N);
+    Run<T, N> r;
+    __builtin_memcpy(&r.v, p, sizeof(T) * N);
+    return r;
 }
-template <typename T> __device__ __forceinline__ void store_run(T* p, const float (&v)[1]) { p[0] = (T)v[0]; }
 
-// ... of which only the first n exist (the others read as 0 and are not written)
+// ... of which only the first n exist; the others read as 0.  Nothing is converted here: what is done with a loaded
+// value waits for it, and loads are to be under way together.
+template <int N, typename T> __device__ __forceinline__ Run<T, N> load_some(const T* p, int n)
+{
+    Run<T, N> r;
+    if (n >= N) {
+        r = load_run<N>(p);
+    } else if constexpr (N == 1) {
+        r.v = (T)0.f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.v[i] = i < n ? p[i] : (T)0.f;
+    }
+    return r;
+}
 template <int N, typename T> __device__ __forceinline__ void load_some(const T* p, int n, float (&v)[N])
 {
-    if (n >= N) {
-        load_run(p, v);
-    } else {
-        for (int i = 0; i < N; ++i) v[i] = i < n ? (float)p[i] : 0.f;
-    }
+    const Run<T, N> r = load_some<N>(p, n);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = r[i];
 }
+
+// v rounded to nearest even; only the first n exist
 template <int N, typename T> __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[N])
 {
-    if (n >= N) {
-        store_run(p, v);
+    if constexpr (N == 1) {
+        if (n > 0) p[0] = (T)v[0];
     } else {
-        for (int i = 0; i < N; ++i)
-            if (i < n) p[i] = (T)v[i];
+        typename Run<T, N>::vt t;
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = (T)v[i];
+        if (n >= N) {
+            __builtin_memcpy(p, &t, sizeof(T) * N);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < n) p[i] = t[i];
+        }
     }
 }
+
+// All waves of the workgroup have come here and their LDS writes are seen.  __syncthreads() would also wait for the global
+// loads that are under way.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 constexpr int kMaxTokens = 1 << 30;      // of a sequence: token numbers and what is added to them fit 32 bits
 constexpr double kMaxElements = 1.1e18; // of a tensor, 2^60: sizes in 64 bits do not overflow
