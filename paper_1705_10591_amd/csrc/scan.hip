@@ -27,19 +27,23 @@ bc_kernel(Rows B, Rows C, int64_t b_g, int64_t c_g, const int* lengths, float* b
 
 // OUT: the outputs of all tokens, with the states wanted on the way; otherwise the states alone, and with `ends` those of each chunk
 // begun at zero (the first at the call's state, which is kept for the second launch in the last chunk's place).
-template <typename T, int W, bool OUT>
-__global__ void __launch_bounds__(kWave * W)
-scan_kernel(ScanParams p, bool ends)
+// WHOLE: the block has 64 channels, so that no run of them is cut.
+template <int W, bool OUT> struct ScanLds {
+    float2 step[kT][kWave];                             // d, d u
+    float ysum[OUT ? W : 1][kT][kWave];
+};
+
+template <typename T, int W, bool OUT, bool WHOLE>
+__device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace& a, ScanLds<W, OUT>& lds, bool ends)
 {
     constexpr int E = kT / W;
-    __shared__ float2 step[kT][kWave];                  // d, d u
-    __shared__ float ysum[OUT ? W : 1][kT][kWave];
-    const ScanPlace a = scan_place(p);
+    auto& step = lds.step;
+    auto& ysum = lds.ysum;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = a.c0 + lane, s0 = wave * kR;
-    const bool ok = lane < a.nc;
+    const bool ok = WHOLE || lane < a.nc;
     // a thread's share of a tile: one token, E channels
-    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = a.nc - tc, ec = a.c0 + tc;
+    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
 
     float A[kR], h[kR] = {}, dtotal = 0.f;
     load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
@@ -72,28 +76,39 @@ scan_kernel(ScanParams p, bool ends)
         if (OUT && p.D) load_some<E>(p.D + ec, nv, skip);
     }
     const bool gate = OUT && p.z.p;
+    int t = a.tile0 * kT + tt;
+    Share<const T, E> pu(p.u, a.n, t, ec), pd(p.delta, a.n, t, ec), pz(p.z, a.n, t, ec);
+    Share<T, E> po(p.out, a.n, t, ec);
     Run<T, E> u{}, dl{}, z{};
-    auto fetch = [&](int tile) {                          // (a token that does not count reads the last that does)
-        if (tile >= a.stop || nv <= 0) return;
-        const int t = min(tile * kT + tt, a.len - 1);
-        u = load_some<E>(p.u.at<const T>(a.n, t, ec), nv);
-        dl = load_some<E>(p.delta.at<const T>(a.n, t, ec), nv);
-        if (gate) z = load_some<E>(p.z.at<const T>(a.n, t, ec), nv);
+    auto fetch = [&](int at) {
+        if (at < a.len && nv > 0) {
+            u = pu.load(nv);
+            dl = pd.load(nv);
+            if (gate) z = pz.load(nv);
+        }
+        pu.forward(); pd.forward(); pz.forward();
     };
-    fetch(a.tile0);
+    if (a.tile0 < a.stop) fetch(t);
     BC bc, next;
     if (a.tile0 < a.stop) bc.load(bc_of(p, a, a.tile0, W, wave));
-    for (int tile = a.tile0; tile < a.stop; ++tile) {
-        const int t = tile * kT + tt;
-        const bool in = t < a.len;
+    for (int tile = a.tile0; tile < a.stop; ++tile, t += kT, po.forward()) {
+        float raw[E], d_[E], u_[E];
+        const Run<T, E> zc = z;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const float raw = dl[i] + dbias[i];
-            const float d = in && i < nv ? (p.softplus ? softplus(raw) : raw) : 0.f;
-            step[tt][tc + i] = make_float2(d, in && i < nv ? d * u[i] : 0.f);
+            raw[i] = dl[i] + dbias[i];
+            u_[i] = u[i];
         }
-        const Run<T, E> uc = u, zc = z;
-        fetch(tile + 1);
+        steps_of(p.softplus, raw, d_);
+        if ((tile + 1) * kT > a.len) {                    // (a sequence's last tile)
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if (t >= a.len) d_[i] = u_[i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) step[tt][tc + i] = make_float2(d_[i], d_[i] * u_[i]);
+        if (tile + 1 < a.stop) fetch(t + kT);
         meet();
         if (p.starts && !ends) store_states(p.starts + lane_states(p, a, (int64_t)a.n * p.tiles + tile, W, wave, lane), h);
         float2 d[kStep], dn[kStep];
@@ -129,19 +144,22 @@ scan_kernel(ScanParams p, bool ends)
             float y[E];
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                y[i] = skip[i] * uc[i];
+                y[i] = skip[i] * u_[i];
 #pragma unroll
                 for (int w = 0; w < W; ++w) y[i] += ysum[w][tt][tc + i];
                 if (gate) y[i] *= zc[i] * sigmoid(zc[i]);
-                if (!in) y[i] = 0.f;
             }
-            store_some<E>(p.out.at<T>(a.n, t, ec), nv, y);
+            if (t >= a.len) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) y[i] = 0.f;
+            }
+            po.store(nv, y);
         }
     }
     if (OUT && nv > 0) {
         const float zero[E] = {};
-        for (int tile = a.stop; tile < a.tile1; ++tile)
-            if (tile * kT + tt < p.L) store_some<E>(p.out.at<T>(a.n, tile * kT + tt, ec), nv, zero);
+        for (int tile = a.stop; tile < a.tile1; ++tile, t += kT, po.forward())       // tiles that do not count
+            if (t < p.L) po.store(nv, zero);
     }
     if (ends) {
         store_states(p.ends + lane_states(p, a, row + a.chunk, W, wave, lane), h);
@@ -149,6 +167,16 @@ scan_kernel(ScanParams p, bool ends)
     } else if (p.state_out && a.chunk == p.chunks - 1 && ok) {
         store_some<kR>(p.state_out + own + s0, p.S - s0, h);
     }
+}
+
+template <typename T, int W, bool OUT>
+__global__ void __launch_bounds__(kWave * W)
+scan_kernel(ScanParams p, bool ends)
+{
+    __shared__ ScanLds<W, OUT> lds;
+    const ScanPlace a = scan_place(p);
+    if (a.nc == kWave) scan_block<T, W, OUT, true>(p, a, lds, ends);
+    else scan_block<T, W, OUT, false>(p, a, lds, ends);
 }
 
 template <typename T, int W>

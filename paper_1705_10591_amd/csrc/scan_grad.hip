@@ -47,49 +47,59 @@ constexpr int kAcross8 = 0x128, kAcross4 = 0x141, kAcross2 = 0x4e, kAcross1 = 0x
 
 // What each chunk but the first leaves of g at its start, begun at zero (the last: at the gradient of the call's last
 // state), and its sum of d.
-template <typename T, int W>
-__global__ void __launch_bounds__(kWave * W)
-scan_back_kernel(ScanParams p)
+template <typename T, int W, bool WHOLE>
+__device__ __forceinline__ void back_block(const ScanParams& p, const ScanPlace& a, float2 (&step)[kT][kWave])   // d, dy
 {
     constexpr int E = kT / W;
-    __shared__ float2 step[kT][kWave];                  // d, dy
-    ScanPlace a = scan_place(p);
-    a.chunk += 1;
-    a.tile0 += p.chunk_tiles;
-    a.tile1 = min(a.tile0 + p.chunk_tiles, p.tiles);
-    a.stop = max(a.tile0, min(a.tile1, (a.len + kT - 1) / kT));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = a.c0 + lane, s0 = wave * kR;
-    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = a.nc - tc, ec = a.c0 + tc;
+    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
     float A[kR], carry[kR] = {}, dtotal = 0.f, dbias[E] = {};
-    load_states(p.A + (int64_t)c * p.S, s0, p.S, lane < a.nc, A);
+    const bool ok = WHOLE || lane < a.nc;
+    load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
 #pragma unroll
     for (int r = 0; r < kR; ++r) A[r] *= kLog2e;
     if (a.chunk == p.chunks - 1 && p.dstate_out)
-        load_states(p.dstate_out + ((int64_t)a.n * p.C + c) * p.S, s0, p.S, lane < a.nc, carry);
+        load_states(p.dstate_out + ((int64_t)a.n * p.C + c) * p.S, s0, p.S, ok, carry);
     if (nv > 0 && p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
+    const bool gate = p.z.p != nullptr;
+    int t = (a.stop - 1) * kT + tt;
+    Share<const T, E> pd(p.delta, a.n, t, ec), pg(p.dout, a.n, t, ec), pz(p.z, a.n, t, ec);
     Run<T, E> dl{}, go{}, z{};
-    auto fetch = [&](int tile) {
-        if (tile < a.tile0 || nv <= 0) return;
-        const int t = min(tile * kT + tt, a.len - 1);
-        dl = load_some<E>(p.delta.at<const T>(a.n, t, ec), nv);
-        go = load_some<E>(p.dout.at<const T>(a.n, t, ec), nv);
-        if (p.z.p) z = load_some<E>(p.z.at<const T>(a.n, t, ec), nv);
+    auto fetch = [&](int at) {
+        if (at < a.len && nv > 0) {
+            dl = pd.load(nv);
+            go = pg.load(nv);
+            if (gate) z = pz.load(nv);
+        }
+        pd.back(); pg.back(); pz.back();
     };
     BC bc, next;
     if (a.stop > a.tile0) {
-        fetch(a.stop - 1);
+        fetch(t);
         bc.load(bc_of(p, a, a.stop - 1, W, wave) + (kT - kStep) / 2);
     }
-    for (int tile = a.stop - 1; tile >= a.tile0; --tile) {
-        const bool in = tile * kT + tt < a.len;
+    for (int tile = a.stop - 1; tile >= a.tile0; --tile, t -= kT) {
+        float raw[E], d_[E], dy[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const float raw = dl[i] + dbias[i];
-            const float d = p.softplus ? softplus(raw) : raw, dy = p.z.p ? go[i] * z[i] * sigmoid(z[i]) : go[i];
-            step[tt][tc + i] = in && i < nv ? make_float2(d, dy) : make_float2(0.f, 0.f);
+            raw[i] = dl[i] + dbias[i];
+            dy[i] = go[i];
         }
-        fetch(tile - 1);
+        steps_of(p.softplus, raw, d_);
+        if (gate) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) dy[i] *= z[i] * sigmoid(z[i]);
+        }
+        if ((tile + 1) * kT > a.len) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if (t >= a.len) d_[i] = dy[i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) step[tt][tc + i] = make_float2(d_[i], dy[i]);
+        if (tile > a.tile0) fetch(t - kT);
         meet();
         float2 d[kStep], dn[kStep];
 #pragma unroll
@@ -121,18 +131,36 @@ scan_back_kernel(ScanParams p)
 }
 
 template <typename T, int W>
-__global__ void __launch_bounds__(kWave * W, 2)
-scan_grad_kernel(ScanParams p)
+__global__ void __launch_bounds__(kWave * W)
+scan_back_kernel(ScanParams p)
+{
+    __shared__ float2 step[kT][kWave];
+    ScanPlace a = scan_place(p);
+    a.chunk += 1;
+    a.tile0 += p.chunk_tiles;
+    a.tile1 = min(a.tile0 + p.chunk_tiles, p.tiles);
+    a.stop = max(a.tile0, min(a.tile1, (a.len + kT - 1) / kT));
+    if (a.nc == kWave) back_block<T, W, true>(p, a, step);
+    else back_block<T, W, false>(p, a, step);
+}
+
+template <int W> struct GradLds {
+    float2 step[kT][kWave];                             // d, d u
+    float gout[kT][kWave];                              // dy
+    float sums[3][W][kT][kWave];                        // over a wave's states: C h, g B, e A
+};
+
+template <typename T, int W, bool WHOLE>
+__device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace& a, GradLds<W>& lds)
 {
     constexpr int E = kT / W;
-    __shared__ float2 step[kT][kWave];                  // d, d u
-    __shared__ float gout[kT][kWave];                   // dy
-    __shared__ float sums[3][W][kT][kWave];             // over a wave's states: C h, g B, e A
-    const ScanPlace a = scan_place(p);
+    auto& step = lds.step;
+    auto& gout = lds.gout;
+    auto& sums = lds.sums;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = a.c0 + lane, s0 = wave * kR;
-    const bool ok = lane < a.nc, gate = p.z.p != nullptr;
-    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = a.nc - tc, ec = a.c0 + tc;
+    const bool ok = WHOLE || lane < a.nc, gate = p.z.p != nullptr;
+    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
 
     float A[kR], carry[kR] = {}, dA[kR] = {};
     load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
@@ -152,49 +180,66 @@ scan_grad_kernel(ScanParams p)
     if (nv > 0) {
         if (p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
         if (p.D) load_some<E>(p.D + ec, nv, skip);
-        const float zero[E] = {};
-        for (int tile = a.stop; tile < a.tile1; ++tile) {            // tiles that do not count
-            const int t = tile * kT + tt;
-            if (t >= p.L) continue;
-            store_some<E>(p.du.at<T>(a.n, t, ec), nv, zero);
-            store_some<E>(p.ddelta.at<T>(a.n, t, ec), nv, zero);
-            if (gate) store_some<E>(p.dz.at<T>(a.n, t, ec), nv, zero);
-        }
     }
+    int t = (a.tile1 - 1) * kT + tt;
+    Share<T, E> qu(p.du, a.n, t, ec), qd(p.ddelta, a.n, t, ec), qz(p.dz, a.n, t, ec);
+    for (int tile = a.tile1 - 1; tile >= a.stop; --tile, t -= kT) {          // tiles that do not count
+        const float zero[E] = {};
+        if (nv > 0 && t < p.L) {
+            qu.store(nv, zero);
+            qd.store(nv, zero);
+            if (gate) qz.store(nv, zero);
+        }
+        qu.back(); qd.back(); qz.back();
+    }
+    Share<const T, E> pu(p.u, a.n, t, ec), pd(p.delta, a.n, t, ec), pg(p.dout, a.n, t, ec), pz(p.z, a.n, t, ec);
     // what a tile reads, asked for a tile ahead
     Run<T, E> un{}, dln{}, gon{}, zn{};
     float hn[kR] = {};
-    auto fetch = [&](int tile) {
-        if (tile < a.tile0) return;
+    auto fetch = [&](int tile, int at) {
         load_states(p.starts + lane_states(p, a, (int64_t)a.n * p.tiles + tile, W, wave, lane), hn);
-        if (nv <= 0) return;
-        const int t = min(tile * kT + tt, a.len - 1);
-        un = load_some<E>(p.u.at<const T>(a.n, t, ec), nv);
-        dln = load_some<E>(p.delta.at<const T>(a.n, t, ec), nv);
-        gon = load_some<E>(p.dout.at<const T>(a.n, t, ec), nv);
-        if (gate) zn = load_some<E>(p.z.at<const T>(a.n, t, ec), nv);
+        if (at < a.len && nv > 0) {
+            un = pu.load(nv);
+            dln = pd.load(nv);
+            gon = pg.load(nv);
+            if (gate) zn = pz.load(nv);
+        }
+        pu.back(); pd.back(); pg.back(); pz.back();
     };
     BC bc, next;
     if (a.stop > a.tile0) {
-        fetch(a.stop - 1);
+        fetch(a.stop - 1, t);
         bc.load(bc_of(p, a, a.stop - 1, W, wave));
     }
-    for (int tile = a.stop - 1; tile >= a.tile0; --tile) {
-        const int t = tile * kT + tt;
-        const bool in = t < a.len && nv > 0;
+    for (int tile = a.stop - 1; tile >= a.tile0; --tile, t -= kT) {
         Run<T, E> u = un, dl = dln, go = gon, z = zn;
         float h0[kR];
 #pragma unroll
         for (int r = 0; r < kR; ++r) h0[r] = hn[r];
+        float raw[E], d_[E], dy_[E], u_[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const float raw = dl[i] + dbias[i];
-            const float d = p.softplus ? softplus(raw) : raw;
-            const bool on = in && i < nv;
-            step[tt][tc + i] = on ? make_float2(d, d * u[i]) : make_float2(0.f, 0.f);
-            gout[tt][tc + i] = !on ? 0.f : gate ? go[i] * z[i] * sigmoid(z[i]) : go[i];
+            raw[i] = dl[i] + dbias[i];
+            u_[i] = u[i];
+            dy_[i] = go[i];
         }
-        fetch(tile - 1);
+        steps_of(p.softplus, raw, d_);
+        if (gate) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) dy_[i] *= z[i] * sigmoid(z[i]);
+        }
+        if ((tile + 1) * kT > a.len) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if (t >= a.len) d_[i] = u_[i] = dy_[i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            step[tt][tc + i] = make_float2(d_[i], d_[i] * u_[i]);
+            gout[tt][tc + i] = dy_[i];
+        }
+        if (tile > a.tile0) fetch(tile - 1, t - kT);
         meet();
         const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, max(tile - 1, a.tile0), W, wave);
         float dec[kT][kR], h[kT][kR];
@@ -280,26 +325,44 @@ scan_grad_kernel(ScanParams p)
             float du[E], dd[E], dz[E];
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                float y = skip[i] * u[i], q = 0.f, ea = 0.f;
+                const float2 s = step[tt][tc + i];
+                const float dy = gout[tt][tc + i], ui = u[i];
+                float y = skip[i] * ui, q = 0.f, ea = 0.f;
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     if (gate) y += sums[0][w][tt][tc + i];
                     q += sums[1][w][tt][tc + i];
                     ea += sums[2][w][tt][tc + i];
                 }
-                const float sg = gate ? sigmoid(z[i]) : 0.f, dy = gate ? go[i] * z[i] * sg : go[i];
-                du[i] = __builtin_fmaf(step[tt][tc + i].x, q, skip[i] * dy);
-                dd[i] = __builtin_fmaf(u[i], q, ea);
-                if (p.softplus) dd[i] *= sigmoid(dl[i] + dbias[i]);
-                dz[i] = gate ? go[i] * y * (sg * (1.f + z[i] * (1.f - sg))) : 0.f;
-                if (!in) du[i] = dd[i] = dz[i] = 0.f;
-                else sumD[i] = __builtin_fmaf(dy, u[i], sumD[i]);
-                sumB[i] += dd[i];
+                du[i] = __builtin_fmaf(s.x, q, skip[i] * dy);
+                dd[i] = __builtin_fmaf(ui, q, ea);
+                dz[i] = y;
+                sumD[i] = __builtin_fmaf(dy, t < a.len ? ui : 0.f, sumD[i]);
             }
-            store_some<E>(p.du.at<T>(a.n, t, ec), nv, du);
-            store_some<E>(p.ddelta.at<T>(a.n, t, ec), nv, dd);
-            if (gate) store_some<E>(p.dz.at<T>(a.n, t, ec), nv, dz);
+            if (p.softplus) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) dd[i] *= sigmoid(dl[i] + dbias[i]);
+            }
+            if (gate) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const float sg = sigmoid(z[i]);
+                    dz[i] *= go[i] * (sg * (1.f + z[i] * (1.f - sg)));
+                }
+            }
+            if ((tile + 1) * kT > a.len) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    if (t >= a.len) du[i] = dd[i] = dz[i] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) sumB[i] += dd[i];
+            qu.store(nv, du);
+            qd.store(nv, dd);
+            if (gate) qz.store(nv, dz);
         }
+        qu.back(); qd.back(); qz.back();
     }
     if (a.chunk == 0 && p.dstate && ok) store_some<kR>(p.dstate + own + s0, p.S - s0, carry);
     store_states(p.part_A + lane_states(p, a, row + a.chunk, W, wave, lane), dA);
@@ -319,6 +382,16 @@ scan_grad_kernel(ScanParams p)
         p.part_D[at] = s.x;
         p.part_bias[at] = s.y;
     }
+}
+
+template <typename T, int W>
+__global__ void __launch_bounds__(kWave * W, 2)
+scan_grad_kernel(ScanParams p)
+{
+    __shared__ GradLds<W> lds;
+    const ScanPlace a = scan_place(p);
+    if (a.nc == kWave) grad_block<T, W, true>(p, a, lds);
+    else grad_block<T, W, false>(p, a, lds);
 }
 
 // dB and dC of 64 values (8 tokens, 4 states) from the parts of a group's channel blocks.

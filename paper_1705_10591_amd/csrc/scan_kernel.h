@@ -97,8 +97,30 @@ __device__ __forceinline__ bc_ptr bc_of(const ScanParams& p, const ScanPlace& a,
     return (bc_ptr)(p.bc) + ((((int64_t)a.n * p.G + a.g) * p.tiles + tile) * W + wave) * (kT / 2);
 }
 
+// d of a run of channels, before the tokens that do not count are masked.
+template <int E> __device__ __forceinline__ void steps_of(bool soft, const float (&raw)[E], float (&d)[E])
+{
+#pragma unroll
+    for (int i = 0; i < E; ++i) d[i] = raw[i];
+    if (!soft) return;
+#pragma unroll
+    for (int i = 0; i < E; ++i) d[i] = softplus(raw[i]);
+}
+
 // Nothing moves past this point: what is written above it is under way before what is written below begins.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// A thread's share of the tiles of a token tensor: one token a tile, E channels.  It walks by whole tiles, so that a tile
+// costs one 64-bit addition.
+template <typename T, int E> struct Share {
+    T* p;
+    int64_t step;
+    __device__ __forceinline__ Share(const Rows& rows, int n, int t, int c) : p(rows.at<T>(n, t, c)), step(rows.l * kT) {}
+    __device__ __forceinline__ void forward() { p += step; }
+    __device__ __forceinline__ void back() { p -= step; }
+    __device__ __forceinline__ auto load(int nv) const { return load_some<E>(p, nv); }
+    __device__ __forceinline__ void store(int nv, const float (&v)[E]) const { store_some<E>(p, nv, v); }
+};
 
 // Index of this lane's four states among those of all channels.
 __device__ __forceinline__ int64_t lane_states(const ScanParams& p, const ScanPlace& a, int64_t row, int W, int wave, int lane)

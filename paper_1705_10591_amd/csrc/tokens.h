@@ -79,14 +79,13 @@ __device__ __forceinline__ float rcp_(float x) { return __builtin_amdgcn_rcpf(x)
 // 1 / (1 + e^-x): exp2 and the reciprocal are good to 1 ulp each, and where e^-x overflows the quotient is 0 as it should be.
 __device__ __forceinline__ float sigmoid(float x) { return rcp_(1.f + exp2_(-kLog2e * x)); }
 
-// log(1 + e^x).  log(w) loses the digits that w = 1 + e rounded away; e * log(w) / (w - 1) has them back, since the
-// quotient log(w) / (w - 1) changes slowly (Goldberg, "What every computer scientist should know about floating-point
-// arithmetic", theorem 4).  Beyond 20 the sum is x to within 2e-9.
+// log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x| at most 1.  w = 1 + e rounds off c = e - (w - 1), up to 2^-24; since
+// log(1 + e) = log(w) + c / w to first order and c (1 - 1 / w) is at most 2^-24 e, adding c itself leaves errors of an ulp,
+// small steps (e << 1, where log(w) has few digits of e) among them.
 __device__ __forceinline__ float softplus(float x)
 {
-    const float e = exp2_(kLog2e * x), w = 1.f + e;
-    const float r = w == 1.f ? e : e * (kLn2 * __builtin_amdgcn_logf(w)) * rcp_(w - 1.f);
-    return x > 20.f ? x : r;
+    const float e = exp2_(-kLog2e * __builtin_fabsf(x)), w = 1.f + e;
+    return fmaxf(x, 0.f) + __builtin_fmaf(kLn2, __builtin_amdgcn_logf(w), e - (w - 1.f));
 }
 
 // Tokens of sequence n that count.
