@@ -220,7 +220,7 @@ bool scan_sizes_ok(const dconv_scan_args& a)
         return false;
     // (sizes in floating point, so that no product overflows)
     if ((double)a.N * a.L * a.C * kMaxStates >= kMaxElements) return false;
-    const ScanPlan pl = scan_plan(a, true);
+    const ScanPlan pl = scan_plan(a, false);             // (a gradient has no more chunks)
     return (double)a.N * pl.blocks * pl.chunks <= 2147483647.0 &&
            (double)a.N * a.G * pl.tiles * kT * pl.waves <= 2147483647.0 * kThreads;
 }
@@ -233,18 +233,22 @@ ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
     pl.gblocks = (pl.group - 1) / kWave + 1;
     pl.blocks = a.G * pl.gblocks;
     pl.tiles = (a.L + kT - 1) / kT;
-    // Chunks: as many as give the chip four workgroups a CU, none shorter than eight tiles.  They cost another launch that
-    // does most of the work again, so there are none where the channels alone give every CU a workgroup.
-    const double alone = (double)a.N * pl.blocks;
+    // Chunks cost another launch that does most of the work again, so there are none where the channels alone give the
+    // chip nearly two waves a SIMD, nor for a few tiles.  Otherwise as many as give it eight (gradients, whose registers let two
+    // be there at a time: four) in chunks of four tiles or more, or half of that in chunks of two.  Measured, S = 16,
+    // us for 1 chunk and those of the rule (sequences x tokens x channels):
+    //   scan      1 x 256 x 2048  41, 26    1 x 4096 x 4096   531, 131    4 x 2048 x 4096  274, 224    8 x 2048 x 4096   352, (407)
+    //   gradient  1 x 256 x 2048 134, 75    1 x 4096 x 4096  1463, 449    4 x 2048 x 4096  928, 799    8 x 2048 x 4096  1261, (1402)
+    const double alone = (double)a.N * pl.blocks * pl.waves;
     pl.chunks = 1;
-    if (alone < 256) {
-        const int want = (int)(1024 / alone), most = pl.tiles / 8;
-        pl.chunks = want < most ? want : most;
+    if (alone < 1792 && pl.tiles >= 6) {
+        const int most = grad ? (int)(4096 / alone) : (int)(8192 / alone);
+        const int longer = most < pl.tiles / 4 ? most : pl.tiles / 4, shorter = most / 2 < pl.tiles / 2 ? most / 2 : pl.tiles / 2;
+        pl.chunks = longer > shorter ? longer : shorter;
         if (pl.chunks < 2) pl.chunks = 1;
     }
     pl.chunk_tiles = (pl.tiles + pl.chunks - 1) / pl.chunks;
     pl.chunks = (pl.tiles + pl.chunk_tiles - 1) / pl.chunk_tiles;
-    (void)grad;
     return pl;
 }
 

@@ -465,15 +465,18 @@ template <typename T> void launch_typed(const dconv_scan_args& a, const ScanPara
 }
 
 // The workspace of a gradient call, in floats: where its parts begin, and how many there are.
-struct GradSpace { int64_t ends, back, dsum, bc_parts, A_parts, D_parts, bias_parts, starts, all; };
+struct GradSpace { int64_t ends, end_sums, back, dsum, bc_parts, A_parts, D_parts, bias_parts, starts, all; };
 
 GradSpace space_of(const dconv_scan_args& a, const ScanPlan& pl)
 {
     const int64_t rows = (int64_t)a.N * pl.chunks * pl.blocks * kWave, states = rows * pl.waves * kR;
+    const ScanPlan fw = scan_plan(a, false);             // of the launches that make the states again
+    const int64_t frows = a.starts || fw.chunks < 2 ? 0 : (int64_t)a.N * fw.chunks * fw.blocks * kWave;
     GradSpace s;
     int64_t at = scan_bc_floats(a, pl);
     auto take = [&](int64_t n) { const int64_t here = at; at += (n + 3) / 4 * 4; return here; };
-    s.ends = take(pl.chunks > 1 ? states : 0);
+    s.ends = take(frows * fw.waves * kR);
+    s.end_sums = take(frows);
     s.back = take(pl.chunks > 1 ? states : 0);
     s.dsum = take(pl.chunks > 1 ? rows : 0);
     s.bc_parts = take((int64_t)pl.blocks * a.N * pl.tiles * 2 * pl.waves * kWave);
@@ -510,15 +513,18 @@ int dconv_scan_grad(const dconv_scan_args* a, void* stream)
     float* ws = (float*)a->workspace;
     ScanParams p = scan_params(*a, pl);
     p.bc = ws;
-    p.ends = ws + s.ends; p.back = ws + s.back; p.dsum = ws + s.dsum;
+    p.back = ws + s.back; p.dsum = ws + s.dsum;
     p.part_bc = ws + s.bc_parts; p.part_A = ws + s.A_parts; p.part_D = ws + s.D_parts; p.part_bias = ws + s.bias_parts;
     rc = launch_scan_bc(*a, pl, ws, st);
     if (rc != DCONV_OK) return rc;
     if (!a->starts) {
-        p.starts = ws + s.starts;
-        ScanParams forward = p;
+        const ScanPlan fw = scan_plan(*a, false);
+        ScanParams forward = scan_params(*a, fw);
         forward.state_out = nullptr;
-        rc = launch_scan_forward(*a, forward, pl, false, st);
+        forward.bc = ws;
+        forward.ends = ws + s.ends; forward.dsum = ws + s.end_sums;
+        p.starts = forward.starts = ws + s.starts;
+        rc = launch_scan_forward(*a, forward, fw, false, st);
         if (rc != DCONV_OK) return rc;
     }
     begin_launch();
