@@ -22,7 +22,13 @@ _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: DTYPE_F32}
 # as a single token takes the GPU.
 _CAUSAL = struct.Struct("8i" + 4 * "4q" + "12q")
 _SCAN = struct.Struct("8i" + 12 * "4q" + "15q")
+# ... of the step forms, which leave most fields empty
+_CAUSAL_STEP = struct.Struct("8i" + "qq16x" * 2 + "64x" + "qq8xq40xq16x")
+_SCAN_STEP = struct.Struct("8i" + "qq16x" * 4 + "qq8xq" * 2 + "192x" + "qqq8xq56xq16x")
 _NONE = (0, 0, 0, 0)
+_INT32, _FLOAT32 = torch.int32, torch.float32
+# (torch.cuda.current_device and a Stream object take as long as all checks of a call)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def declare(lib: ctypes.CDLL) -> None:
@@ -36,59 +42,92 @@ def declare(lib: ctypes.CDLL) -> None:
             fn.restype = ctypes.c_int
 
 
+_loaded = None
+
+
 def _lib():
-    from . import load_library
-    return load_library()
+    global _loaded
+    if _loaded is None:
+        from . import load_library
+        _loaded = load_library()
+    return _loaded
 
 
 def _run(fn, index, args):
-    from . import _enqueue
-    _enqueue(fn, index, args)
+    from . import _enqueue, _raise, _raw_stream
+    if index != _device():
+        return _enqueue(fn, index, args)
+    rc = fn(args, _raw_stream(index))
+    if rc:
+        _raise(rc)
+
+
+def _bad_shape():
+    from . import STATUS_BAD_SHAPE, _raise
+    _raise(STATUS_BAD_SHAPE)
 
 
 def _first(t, dims, what):
-    """Type, device and sizes that the other tensors of a call have to agree with."""
+    """Type, its number, and device that the other tensors of a call have to agree with."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _DTYPES and t.dim() == dims):
         raise TypeError(f"{what} must be a float16, bfloat16 or float32 CUDA tensor with {dims} dims")
     if 0 in t.shape:
-        from . import STATUS_BAD_SHAPE, _raise
-        _raise(STATUS_BAD_SHAPE)
-    return t.dtype, t.get_device()
+        _bad_shape()
+    return t.dtype, _DTYPES[t.dtype], t.get_device()
 
 
-def _like(t, shape, dtype, index, what):
+def _refuse(t, shape, dtype, index, what):
+    """Says what does not fit."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
         raise TypeError(f"{what} must be a CUDA tensor of type {dtype}")
     if t.get_device() != index:
         raise ValueError(f"{what} is on another device")
-    if t.shape != shape:
-        raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
 
 
-def _rows(t, shape, dtype, index, what, out=False):
+def _fits(t, shape, dtype, index, what):
+    try:
+        if t.dtype is dtype and t.get_device() == index and t.shape == shape:
+            return
+    except AttributeError:
+        pass
+    _refuse(t, shape, dtype, index, what)
+
+
+def _row(t, shape, dtype, index, what):
+    """(pointer, stride) of the rows of a step's token tensor."""
+    _fits(t, shape, dtype, index, what)
+    s = t.stride()
+    if s[1] != 1 and shape[1] != 1:
+        raise TypeError(f"the last dimension of {what} must be contiguous")
+    return t.data_ptr(), s[0]
+
+
+def _rows(t, shape, dtype, index, what):
     """(pointer, strides of sequence, token and group) of a token tensor."""
     if t is None:
         return _NONE
-    _like(t, shape, dtype, index, what)
+    _fits(t, shape, dtype, index, what)
     s = t.stride()
     if s[-1] != 1 and shape[-1] != 1:
         raise TypeError(f"the last dimension of {what} must be contiguous")
-    strides = {2: (s[0], 0, 0), 3: (s[0], s[1], 0), 4: s[:3]}[len(shape)]
-    if out:
-        # tokens that share memory would be written by several workgroups
-        span = shape[-1]
-        for stride, size in sorted(zip(s[:-1], shape[:-1])):
-            if size > 1:
-                if stride < span:
-                    raise ValueError(f"elements of {what} overlap")
-                span += stride * (size - 1)
-    return (t.data_ptr(), *strides)
+    return (t.data_ptr(), s[0], s[1], s[2] if len(s) == 4 else 0)
+
+
+def _apart(t, what):
+    """Refuses an output whose tokens share memory: they would be written by several workgroups."""
+    span = t.shape[-1]
+    for stride, size in sorted(zip(t.stride()[:-1], t.shape[:-1])):
+        if size > 1:
+            if stride < span:
+                raise ValueError(f"elements of {what} overlap")
+            span += stride * (size - 1)
 
 
 def _dense(t, shape, dtype, index, what):
     if t is None:
         return 0
-    _like(t, shape, dtype, index, what)
+    _fits(t, shape, dtype, index, what)
     if not t.is_contiguous():
         raise TypeError(f"{what} must be contiguous")
     return t.data_ptr()
@@ -96,11 +135,12 @@ def _dense(t, shape, dtype, index, what):
 
 def _cache(t, tail, dtype, index, what, rows, slots):
     """(pointer, rows) of a cache of states that a step updates."""
-    if not isinstance(t, torch.Tensor) or t.dim() != len(tail) + 1 or tuple(t.shape[1:]) != tuple(tail):
+    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.shape[1:] != tail:
         raise ValueError(f"{what} must have the shape (rows, {', '.join(map(str, tail))})")
-    if t.shape[0] == 0 or (slots is None and t.shape[0] < rows):
+    M = t.shape[0]
+    if M == 0 or (slots is None and M < rows):
         raise ValueError(f"{what} has too few rows")
-    return _dense(t, t.shape, dtype, index, what), t.shape[0]
+    return _dense(t, (M, *tail), dtype, index, what), M
 
 
 def _workspace(bytes_, index):
@@ -137,15 +177,18 @@ def dconv_causal(x: torch.Tensor, filt: torch.Tensor, bias: torch.Tensor | None 
     x [N,L,C], filt [C,F] (F <= 8), bias [C], all of one type.  state [N,F-1,C]: the rows before token 0 (default: zeros);
     state_out, which may be `state`, receives the last F-1 rows of each sequence.  lengths [N] int32: the tokens of each
     sequence that count; out is 0 behind them."""
-    dtype, index = _first(x, 3, "x")
+    dtype, code, index = _first(x, 3, "x")
     N, L, C = x.shape
     F = _taps(filt, C)
     if out is None:
-        out = torch.empty((N, L, C), dtype=dtype, device=x.device)
+        out = x.new_empty((N, L, C))
+    else:
+        _fits(out, x.shape, dtype, index, "out")
+        _apart(out, "out")
     rows = (N, F - 1, C)
     args = _CAUSAL.pack(
-        _DTYPES[dtype], N, L, C, F, 0, bool(silu), 0,
-        *_rows(x, (N, L, C), dtype, index, "x"), *_rows(out, (N, L, C), dtype, index, "out", True), *_NONE, *_NONE,
+        code, N, L, C, F, 0, bool(silu), 0,
+        *_rows(x, (N, L, C), dtype, index, "x"), *_rows(out, (N, L, C), dtype, index, "out"), *_NONE, *_NONE,
         _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
         _dense(state, rows, dtype, index, "state"), _dense(state_out, rows, dtype, index, "state_out"), 0, 0, 0, 0,
         _dense(lengths, (N,), torch.int32, index, "lengths"), 0, 0, 0)
@@ -159,19 +202,22 @@ def dconv_causal_grad(dout: torch.Tensor, x: torch.Tensor, filt: torch.Tensor, b
     """Gradients of dconv_causal(x, filt, bias, ...) from dout, the gradient of its output, and dstate_out, that of state_out.
 
     dx may be given (a slice of a wider gradient, say); it is 0 behind `lengths`.  dstate is None without a state."""
-    dtype, index = _first(x, 3, "x")
+    dtype, code, index = _first(x, 3, "x")
     N, L, C = x.shape
     F = _taps(filt, C)
     rows = (N, F - 1, C)
     if dx is None:
-        dx = torch.empty((N, L, C), dtype=dtype, device=x.device)
+        dx = x.new_empty((N, L, C))
+    else:
+        _fits(dx, x.shape, dtype, index, "dx")
+        _apart(dx, "dx")
     sums = torch.empty(C * (F + 1), dtype=torch.float32, device=x.device)
     dfilt, dbias = sums[:C * F].view(C, F), sums[C * F:]
     dstate = None if state is None else torch.empty(rows, dtype=dtype, device=x.device)
     fn = _lib()
-    head = (_DTYPES[dtype], N, L, C, F, 0, bool(silu), 0,
+    head = (code, N, L, C, F, 0, bool(silu), 0,
             *_rows(x, (N, L, C), dtype, index, "x"), *_NONE, *_rows(dout, (N, L, C), dtype, index, "dout"),
-            *_rows(dx, (N, L, C), dtype, index, "dx", True),
+            *_rows(dx, (N, L, C), dtype, index, "dx"),
             _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
             _dense(state, rows, dtype, index, "state"), 0, _dense(dstate_out, rows, dtype, index, "dstate_out"),
             0 if dstate is None else dstate.data_ptr(), dfilt.data_ptr(), dbias.data_ptr(),
@@ -188,18 +234,20 @@ def dconv_causal_step(x: torch.Tensor, state: torch.Tensor, filt: torch.Tensor, 
 
     slots [N] int32: the window of each row (default: row n has window n); rows with a slot outside the cache, or
     one that an earlier row has, are padding: out is 0 there and no window changes."""
-    dtype, index = _first(x, 2, "x")
+    dtype, code, index = _first(x, 2, "x")
     N, C = x.shape
     F = _taps(filt, C)
     if out is None:
-        out = torch.empty((N, C), dtype=dtype, device=x.device)
+        out = x.new_empty((N, C))
+        o = out.data_ptr(), C
+    else:
+        o = _row(out, x.shape, dtype, index, "out")
+        _apart(out, "out")
     cache, M = _cache(state, (F - 1, C), dtype, index, "state", N, slots)
-    args = _CAUSAL.pack(
-        _DTYPES[dtype], N, 1, C, F, M, bool(silu), 0,
-        *_rows(x, (N, C), dtype, index, "x"), *_rows(out, (N, C), dtype, index, "out", True), *_NONE, *_NONE,
-        _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"), 0, cache, 0, 0, 0, 0,
-        0, _dense(slots, (N,), torch.int32, index, "slots"), 0, 0)
-    _run(_lib().dconv_causal_step, index, args)
+    _run(_lib().dconv_causal_step, index, _CAUSAL_STEP.pack(
+        code, N, 1, C, F, M, bool(silu), 0, *_row(x, x.shape, dtype, index, "x"), *o,
+        _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"), cache,
+        _dense(slots, (N,), _INT32, index, "slots")))
     return out
 
 
@@ -210,12 +258,12 @@ def _taps(filt, C):
 
 
 def _scan_sizes(u, A, B, dims):
-    dtype, index = _first(u, dims, "u")
+    dtype, code, index = _first(u, dims, "u")
     if not isinstance(A, torch.Tensor) or A.dim() != 2 or A.shape[0] != u.shape[-1]:
         raise ValueError("A must have the shape (C, S)")
     if not isinstance(B, torch.Tensor) or B.dim() != dims + 1:
         raise ValueError(f"B must have {dims + 1} dims")
-    return dtype, index, A.shape[1], B.shape[-2]
+    return dtype, code, index, A.shape[1], B.shape[-2]
 
 
 def _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index):
@@ -232,8 +280,7 @@ def scan_starts(N: int, L: int, C: int, S: int, G: int = 1, device="cuda") -> to
     """An empty tensor for the `starts` of dconv_scan and dconv_scan_grad on sequences of these sizes."""
     need = _lib().dconv_scan_starts(_SCAN.pack(DTYPE_F32, N, L, C, S, G, 0, 0, *(12 * _NONE), *(15 * (0,))))
     if need < 0:
-        from . import STATUS_BAD_SHAPE, _raise
-        _raise(STATUS_BAD_SHAPE)
+        _bad_shape()
     return torch.empty(need // 4, dtype=torch.float32, device=device)
 
 
@@ -256,14 +303,17 @@ def dconv_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.T
     D and delta_bias [C], fp32.  state [N,C,S] fp32: h before token 0 (default: zeros); state_out, which may be `state`,
     receives h behind the last token.  lengths [N] int32: the tokens that count; out is 0 behind them.
     starts (of scan_starts): receives what lets dconv_scan_grad go back without running the scan again."""
-    dtype, index, S, G = _scan_sizes(u, A, B, 3)
+    dtype, code, index, S, G = _scan_sizes(u, A, B, 3)
     N, L, ch = u.shape
     wide, narrow = (N, L, ch), (N, L, G, S)
     tokens, bc, params = _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index)
     if out is None:
-        out = torch.empty(wide, dtype=dtype, device=u.device)
-    head = (_DTYPES[dtype], N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
-            *_rows(out, wide, dtype, index, "out", True), *bc[0], *bc[1], *(6 * _NONE), *params,
+        out = u.new_empty(wide)
+    else:
+        _fits(out, wide, dtype, index, "out")
+        _apart(out, "out")
+    head = (code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
+            *_rows(out, wide, dtype, index, "out"), *bc[0], *bc[1], *(6 * _NONE), *params,
             _dense(state, (N, ch, S), torch.float32, index, "state"),
             _dense(state_out, (N, ch, S), torch.float32, index, "state_out"), 0, 0, 0, 0, 0,
             _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), torch.int32, index, "lengths"), 0)
@@ -284,11 +334,15 @@ def dconv_scan_grad(dout: torch.Tensor, u: torch.Tensor, delta: torch.Tensor, A:
 
     starts: what dconv_scan left there for the same inputs; without it the states are made again.  du, ddelta and dz may be
     given (slices of a wider gradient, say); gradients are 0 behind `lengths`."""
-    dtype, index, S, G = _scan_sizes(u, A, B, 3)
+    dtype, code, index, S, G = _scan_sizes(u, A, B, 3)
     N, L, ch = u.shape
     wide, narrow = (N, L, ch), (N, L, G, S)
     tokens, bc, params = _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index)
     make = lambda shape, t=dtype: torch.empty(shape, dtype=t, device=u.device)
+    for t, what in ((du, "du"), (ddelta, "ddelta"), (dz, "dz")):
+        if t is not None:
+            _fits(t, wide, dtype, index, what)
+            _apart(t, what)
     du = make(wide) if du is None else du
     ddelta = make(wide) if ddelta is None else ddelta
     if z is None:
@@ -300,9 +354,9 @@ def dconv_scan_grad(dout: torch.Tensor, u: torch.Tensor, delta: torch.Tensor, A:
     dbias = None if delta_bias is None else make((ch,), torch.float32)
     dstate = None if state is None else make((N, ch, S), torch.float32)
     ptr = lambda t: 0 if t is None else t.data_ptr()
-    head = (_DTYPES[dtype], N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2], *_NONE, *bc[0], *bc[1],
-            *_rows(dout, wide, dtype, index, "dout"), *_rows(du, wide, dtype, index, "du", True),
-            *_rows(ddelta, wide, dtype, index, "ddelta", True), *_rows(dz, wide, dtype, index, "dz", True),
+    head = (code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2], *_NONE, *bc[0], *bc[1],
+            *_rows(dout, wide, dtype, index, "dout"), *_rows(du, wide, dtype, index, "du"),
+            *_rows(ddelta, wide, dtype, index, "ddelta"), *_rows(dz, wide, dtype, index, "dz"),
             *_rows(dB, narrow, dtype, index, "dB"), *_rows(dC, narrow, dtype, index, "dC"), *params,
             _dense(state, (N, ch, S), torch.float32, index, "state"), 0,
             _dense(dstate_out, (N, ch, S), torch.float32, index, "dstate_out"), ptr(dstate), ptr(dA), ptr(dD), ptr(dbias),
@@ -321,22 +375,20 @@ def dconv_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: to
     """One token of each row: u, delta, z [N,C], B, C [N,G,S]; out [N,C], and `state` [M,C,S] (fp32) is updated.
 
     slots as for dconv_causal_step."""
-    dtype, index, S, G = _scan_sizes(u, A, B, 2)
+    dtype, code, index, S, G = _scan_sizes(u, A, B, 2)
     N, ch = u.shape
     wide, narrow = (N, ch), (N, G, S)
     if out is None:
-        out = torch.empty(wide, dtype=dtype, device=u.device)
-    tokens = [_rows(t, wide, dtype, index, what) for t, what in ((u, "u"), (delta, "delta"), (z, "z"))]
-    bc = []
-    for t, what in ((B, "B"), (C, "C")):                       # [N, G, S]: the middle stride is the groups'
-        p, sn, sg, _ = _rows(t, narrow, dtype, index, what)
-        bc.append((p, sn, 0, sg))
-    cache, M = _cache(state, (ch, S), torch.float32, index, "state", N, slots)
-    args = _SCAN.pack(
-        _DTYPES[dtype], N, 1, ch, S, G, M, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
-        *_rows(out, wide, dtype, index, "out", True), *bc[0], *bc[1], *(6 * _NONE),
-        _dense(A, (ch, S), torch.float32, index, "A"), _dense(D, (ch,), torch.float32, index, "D"),
-        _dense(delta_bias, (ch,), torch.float32, index, "delta_bias"), 0, cache, 0, 0, 0, 0, 0, 0, 0,
-        _dense(slots, (N,), torch.int32, index, "slots"), 0, 0)
-    _run(_lib().dconv_scan_step, index, args)
+        out = u.new_empty(wide)
+        o = out.data_ptr(), ch
+    else:
+        o = _row(out, wide, dtype, index, "out")
+        _apart(out, "out")
+    b, c = _rows(B, narrow, dtype, index, "B"), _rows(C, narrow, dtype, index, "C")      # the second stride is the groups'
+    cache, M = _cache(state, (ch, S), _FLOAT32, index, "state", N, slots)
+    _run(_lib().dconv_scan_step, index, _SCAN_STEP.pack(
+        code, N, 1, ch, S, G, M, bool(softplus), *_row(u, wide, dtype, index, "u"), *_row(delta, wide, dtype, index, "delta"),
+        *((0, 0) if z is None else _row(z, wide, dtype, index, "z")), *o, *b[:3], *c[:3],
+        _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
+        _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"), cache, _dense(slots, (N,), _INT32, index, "slots")))
     return out

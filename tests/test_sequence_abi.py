@@ -191,3 +191,14 @@ def test_python_functions_refuse_what_does_not_fit():
         with pytest.raises(error):
             call()
             pytest.fail(f"call {k} was taken")
+
+
+def test_step_structs_lay_their_fields_where_the_full_ones_have_them():
+    v = list(range(1, 17))
+    full = {"dtype": 1, "N": 2, "L": 3, "C": 4, "F": 5, "M": 6, "silu": 7, "reserved": 8, "x.p": 9, "x.sn": 10, "out.p": 11, "out.sn": 12,
+            "filt": 13, "bias": 14, "state_out": 15, "slots": 16}
+    assert q._CAUSAL_STEP.pack(*v) == _pack(CAUSAL, q._CAUSAL, full)
+    names = ["dtype", "N", "L", "C", "S", "G", "M", "softplus", "u.p", "u.sn", "delta.p", "delta.sn", "z.p", "z.sn", "out.p", "out.sn",
+             "B.p", "B.sn", "B.sg", "Cm.p", "Cm.sn", "Cm.sg", "A", "D", "delta_bias", "state_out", "slots"]
+    v = list(range(1, len(names) + 1))
+    assert q._SCAN_STEP.pack(*v) == _pack(SCAN, q._SCAN, dict(zip(names, v)))
