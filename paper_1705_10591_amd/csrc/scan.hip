@@ -5,68 +5,71 @@ namespace dconv {
 
 namespace {
 
-// B and C of a token and wave, side by side in fp32: thread i has the i-th eight of the layout.
+// B and C in fp32 as the scans read them: thread i has token i % 16 of a wave and tile.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 bc_kernel(Rows B, Rows C, int64_t b_g, int64_t c_g, const int* lengths, float* bc, int N, int L, int G, int S, int W,
-          int tiles)
+          int R, int tiles)
 {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const int64_t unit = i / kT, tile = unit / W, seq = tile / tiles;
-    const int s0 = (int)(unit - tile * W) * kR;
+    const int s0 = (int)(unit - tile * W) * R, ns = min(R, S - s0);
     const int t = (int)(tile - seq * tiles) * kT + (int)(i - unit * kT), n = (int)(seq / G), g = (int)(seq - (int64_t)n * G);
     if (n >= N) return;
     float b[kR] = {}, c[kR] = {};
     if (t < length_of(lengths, n, L)) {
-        load_some<kR>(B.at<const T>(n, t, 0) + g * b_g + s0, S - s0, b);
-        if (C.p) load_some<kR>(C.at<const T>(n, t, 0) + g * c_g + s0, S - s0, c);
+        load_some<kR>(B.at<const T>(n, t, 0) + g * b_g + s0, ns, b);
+        if (C.p) load_some<kR>(C.at<const T>(n, t, 0) + g * c_g + s0, ns, c);
     }
-    store_states(bc + i * 8, b);
-    store_states(bc + i * 8 + kR, c);
+    float* to = bc + (i & ~(int64_t)1) * 8 + (i & 1) * kR;
+    store_states(to, b);
+    store_states(to + 2 * kR, c);
 }
 
 // OUT: the outputs of all tokens, with the states wanted on the way; otherwise the states alone, and with `ends` those of each chunk
 // begun at zero (the first at the call's state, which is kept for the second launch in the last chunk's place).
 // WHOLE: the block has 64 channels, so that no run of them is cut.
-template <int W, bool OUT> struct ScanLds {
-    float2 step[kT][kWave];                             // d, d u
-    float ysum[OUT ? W : 1][kT][kWave];
+// AHEAD: while a tile's recurrence runs, the one before it is finished (sums over waves, gate, store) and the one after it
+// prepared (d, d u): two of everything in LDS, one barrier a tile, and work between the recurrence's dependent
+// instructions.  That is for launches of few waves; where there are many, they fill each other's gaps and twice
+// the LDS would keep some of them away.
+template <int W, bool OUT, bool AHEAD> struct ScanLds {
+    float2 step[AHEAD ? 2 : 1][kT][kWave];              // d, d u
+    float ysum[AHEAD && OUT ? 2 : 1][OUT ? W : 1][kT][kWave];
 };
 
-template <typename T, int W, bool OUT, bool WHOLE>
-__device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace& a, ScanLds<W, OUT>& lds, bool ends)
+template <typename T, int W, int R, bool OUT, bool AHEAD, bool WHOLE>
+__device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace& a, ScanLds<W, OUT, AHEAD>& lds, bool ends)
 {
     constexpr int E = kT / W;
-    auto& step = lds.step;
-    auto& ysum = lds.ysum;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c = a.c0 + lane, s0 = wave * kR;
+    const int c = a.c0 + lane, s0 = wave * R;
     const bool ok = WHOLE || lane < a.nc;
     // a thread's share of a tile: one token, E channels
     const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
 
-    float A[kR], h[kR] = {}, dtotal = 0.f;
+    float A[R], h[R] = {}, dtotal = 0.f;
     load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
 #pragma unroll
-    for (int r = 0; r < kR; ++r) A[r] *= kLog2e;
+    for (int r = 0; r < R; ++r) A[r] *= kLog2e;
     const int64_t own = ((int64_t)a.n * p.C + c) * p.S;
     const int64_t row = (int64_t)a.n * p.chunks;
     if (ends) {
         if (a.chunk == 0) {
             if (p.state) load_states(p.state + own, s0, p.S, ok, h);
-            store_states(p.ends + lane_states(p, a, row + p.chunks - 1, W, wave, lane), h);
+            store_states(p.ends + lane_states<W, R>(p, a, row + p.chunks - 1, wave, lane), h);
         }
     } else if (p.chunks == 1) {
         if (p.state) load_states(p.state + own, s0, p.S, ok, h);
     } else if (a.chunk == 0) {
-        load_states(p.ends + lane_states(p, a, row + p.chunks - 1, W, wave, lane), h);
+        load_states(p.ends + lane_states<W, R>(p, a, row + p.chunks - 1, wave, lane), h);
     } else {
         for (int k = 0; k < a.chunk; ++k) {
-            float e[kR];
-            load_states(p.ends + lane_states(p, a, row + k, W, wave, lane), e);
+            float e[R];
+            load_states(p.ends + lane_states<W, R>(p, a, row + k, wave, lane), e);
             const float d = p.dsum[((row + k) * p.blocks + a.block) * kWave + lane];
 #pragma unroll
-            for (int r = 0; r < kR; ++r) h[r] = __builtin_fmaf(exp2_(d * A[r]), h[r], e[r]);
+            for (int r = 0; r < R; ++r) h[r] = __builtin_fmaf(exp2_(d * A[r]), h[r], e[r]);
         }
     }
 
@@ -76,10 +79,11 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
         if (OUT && p.D) load_some<E>(p.D + ec, nv, skip);
     }
     const bool gate = OUT && p.z.p;
-    int t = a.tile0 * kT + tt;
+    int t = a.tile0 * kT + tt;                            // of this thread in the tile at hand
     Share<const T, E> pu(p.u, a.n, t, ec), pd(p.delta, a.n, t, ec), pz(p.z, a.n, t, ec);
     Share<T, E> po(p.out, a.n, t, ec);
-    Run<T, E> u{}, dl{}, z{};
+    pu.spare(); pd.spare(); pz.spare(); po.spare();
+    Run<T, E> u{}, dl{}, z{}, uc{}, zc{}, ul{}, zl{};     // of the tile fetched, the one at hand, the last one
     auto fetch = [&](int at) {
         if (at < a.len && nv > 0) {
             u = pu.load(nv);
@@ -88,12 +92,8 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
         }
         pu.forward(); pd.forward(); pz.forward();
     };
-    if (a.tile0 < a.stop) fetch(t);
-    BC bc, next;
-    if (a.tile0 < a.stop) bc.load(bc_of(p, a, a.tile0, W, wave));
-    for (int tile = a.tile0; tile < a.stop; ++tile, t += kT, po.forward()) {
+    auto prepare = [&](int tile, int at) {                // the tile fetched, for the loop
         float raw[E], d_[E], u_[E];
-        const Run<T, E> zc = z;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             raw[i] = dl[i] + dbias[i];
@@ -103,14 +103,59 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
         if ((tile + 1) * kT > a.len) {                    // (a sequence's last tile)
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                if (t >= a.len) d_[i] = u_[i] = 0.f;
+                if (at >= a.len) d_[i] = u_[i] = 0.f;
             }
         }
 #pragma unroll
-        for (int i = 0; i < E; ++i) step[tt][tc + i] = make_float2(d_[i], d_[i] * u_[i]);
-        if (tile + 1 < a.stop) fetch(t + kT);
-        meet();
-        if (p.starts && !ends) store_states(p.starts + lane_states(p, a, (int64_t)a.n * p.tiles + tile, W, wave, lane), h);
+        for (int i = 0; i < E; ++i) lds.step[AHEAD ? tile & 1 : 0][tt][tc + i] = make_float2(d_[i], d_[i] * u_[i]);
+    };
+    auto finish = [&](int tile, int at) {                 // the last tile
+        if (!OUT) return;
+        if (nv > 0 && at < p.L) {
+            float y[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) y[i] = skip[i] * ul[i];
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const Run<float, E> part = lds_run<E>(&lds.ysum[AHEAD && OUT ? tile & 1 : 0][w][tt][tc]);
+#pragma unroll
+                for (int i = 0; i < E; ++i) y[i] += part[i];
+            }
+            if (gate) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) y[i] *= zl[i] * sigmoid(zl[i]);
+            }
+            if ((tile + 1) * kT > a.len) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    if (at >= a.len) y[i] = 0.f;
+                }
+            }
+            po.store(nv, y);
+        }
+        po.forward();
+    };
+    BC<OUT> bc, next;
+    if (a.tile0 < a.stop) {
+        fetch(t);
+        bc.load(bc_of(p, a, a.tile0, W, wave));
+        if (AHEAD) {
+            prepare(a.tile0, t);
+            uc = u; zc = z;
+            if (a.tile0 + 1 < a.stop) fetch(t + kT);
+            meet();
+        }
+    }
+    for (int tile = a.tile0; tile < a.stop; ++tile, t += kT) {
+        const auto& step = lds.step[AHEAD ? tile & 1 : 0];
+        auto& ysum = lds.ysum[AHEAD && OUT ? tile & 1 : 0];
+        if (!AHEAD) {
+            prepare(tile, t);
+            ul = u; zl = z;
+            if (tile + 1 < a.stop) fetch(t + kT);
+            meet();
+        }
+        if (p.starts && !ends) store_states(p.starts + lane_states<W, R>(p, a, (int64_t)a.n * p.tiles + tile, wave, lane), h);
         float2 d[kStep], dn[kStep];
 #pragma unroll
         for (int k = 0; k < kStep; ++k) d[k] = step[k][lane];
@@ -118,16 +163,18 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
 #pragma unroll
         for (int k0 = 0; k0 < kT; k0 += kStep) {
             const bool more = k0 + kStep < kT;
-            next.load(more ? here + (k0 + kStep) / 2 : after);
+            next.load(more ? here + k0 + kStep : after);
 #pragma unroll
             for (int k = 0; k < kStep; ++k)
                 if (more) dn[k] = step[k0 + kStep + k][lane];
             in_order();
+            if (AHEAD && k0 == 0 && tile > a.tile0) finish(tile - 1, t - kT);
+            if (AHEAD && k0 == 2 * kStep && tile + 1 < a.stop) prepare(tile + 1, t + kT);
 #pragma unroll
             for (int k = 0; k < kStep; ++k) {
                 float y = 0.f;
 #pragma unroll
-                for (int r = 0; r < kR; ++r) {
+                for (int r = 0; r < R; ++r) {
                     h[r] = __builtin_fmaf(exp2_(d[k].x * A[r]), h[r], d[k].y * bc.b(k, r));
                     if (OUT) y = r ? __builtin_fmaf(bc.c(k, r), h[r], y) : bc.c(k, r) * h[r];
                 }
@@ -139,72 +186,68 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
 #pragma unroll
             for (int k = 0; k < kStep; ++k) d[k] = dn[k];
         }
-        meet();
-        if (OUT && nv > 0 && t < p.L) {
-            float y[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                y[i] = skip[i] * u_[i];
-#pragma unroll
-                for (int w = 0; w < W; ++w) y[i] += ysum[w][tt][tc + i];
-                if (gate) y[i] *= zc[i] * sigmoid(zc[i]);
-            }
-            if (t >= a.len) {
-#pragma unroll
-                for (int i = 0; i < E; ++i) y[i] = 0.f;
-            }
-            po.store(nv, y);
+        if (AHEAD) {
+            ul = uc; zl = zc;
+            uc = u; zc = z;
+            if (tile + 2 < a.stop) fetch(t + 2 * kT);
+            meet();
+        } else {
+            meet();
+            finish(tile, t);
         }
     }
+    if (AHEAD && a.tile0 < a.stop) finish(a.stop - 1, t - kT);
     if (OUT && nv > 0) {
         const float zero[E] = {};
         for (int tile = a.stop; tile < a.tile1; ++tile, t += kT, po.forward())       // tiles that do not count
             if (t < p.L) po.store(nv, zero);
     }
     if (ends) {
-        store_states(p.ends + lane_states(p, a, row + a.chunk, W, wave, lane), h);
+        store_states(p.ends + lane_states<W, R>(p, a, row + a.chunk, wave, lane), h);
         if (wave == 0) p.dsum[((row + a.chunk) * p.blocks + a.block) * kWave + lane] = dtotal;
     } else if (p.state_out && a.chunk == p.chunks - 1 && ok) {
-        store_some<kR>(p.state_out + own + s0, p.S - s0, h);
+        store_some<R>(p.state_out + own + s0, p.S - s0, h);
     }
 }
 
-template <typename T, int W, bool OUT>
+template <typename T, int W, int R, bool OUT, bool AHEAD>
 __global__ void __launch_bounds__(kWave * W)
 scan_kernel(ScanParams p, bool ends)
 {
-    __shared__ ScanLds<W, OUT> lds;
+    __shared__ ScanLds<W, OUT, AHEAD> lds;
     const ScanPlace a = scan_place(p);
-    if (a.nc == kWave) scan_block<T, W, OUT, true>(p, a, lds, ends);
-    else scan_block<T, W, OUT, false>(p, a, lds, ends);
+    if (a.nc == kWave) scan_block<T, W, R, OUT, AHEAD, true>(p, a, lds, ends);
+    else scan_block<T, W, R, OUT, AHEAD, false>(p, a, lds, ends);
 }
 
-template <typename T, int W>
+template <typename T, int W, int R>
 void launch_kernel(const ScanParams& p, bool out, bool ends, int64_t blocks, hipStream_t st)
 {
-    if (out)
-        hipLaunchKernelGGL((scan_kernel<T, W, true>), dim3((unsigned)blocks), dim3(kWave * W), 0, st, p, false);
-    else
-        hipLaunchKernelGGL((scan_kernel<T, W, false>), dim3((unsigned)blocks), dim3(kWave * W), 0, st, p, ends);
+    const dim3 grid((unsigned)blocks), threads(kWave * W);
+    // Measured, 16 states, us ahead and not: 64 workgroups of 64 tiles 110, 134; 512 of 128 324, 344; 768 426, 451; 1024 583, 555;
+    // 4 states: 512 of 64 118, 123; 1024 255, 177.
+    const bool ahead = blocks * W < (R == 4 ? 3584 : 3072);
+    if (out && ahead) hipLaunchKernelGGL((scan_kernel<T, W, R, true, true>), grid, threads, 0, st, p, false);
+    else if (out) hipLaunchKernelGGL((scan_kernel<T, W, R, true, false>), grid, threads, 0, st, p, false);
+    else if (ahead) hipLaunchKernelGGL((scan_kernel<T, W, R, false, true>), grid, threads, 0, st, p, ends);
+    else hipLaunchKernelGGL((scan_kernel<T, W, R, false, false>), grid, threads, 0, st, p, ends);
 }
 
 template <typename T>
-void launch_waves(const ScanParams& p, int W, bool out, bool ends, int64_t blocks, hipStream_t st)
+void launch_states(const ScanParams& p, bool out, bool ends, int64_t blocks, hipStream_t st)
 {
-    switch (W) {
-    case 1: return launch_kernel<T, 1>(p, out, ends, blocks, st);
-    case 2: return launch_kernel<T, 2>(p, out, ends, blocks, st);
-    case 4: return launch_kernel<T, 4>(p, out, ends, blocks, st);
-    default: return launch_kernel<T, 8>(p, out, ends, blocks, st);
-    }
+    if (p.S <= 4) launch_kernel<T, 4, 1>(p, out, ends, blocks, st);
+    else if (p.S <= 8) launch_kernel<T, 4, 2>(p, out, ends, blocks, st);
+    else if (p.S <= 16) launch_kernel<T, 4, 4>(p, out, ends, blocks, st);
+    else launch_kernel<T, 8, 4>(p, out, ends, blocks, st);
 }
 
-void launch_typed(const ScanParams& p, int dtype, int W, bool out, bool ends, int64_t blocks, hipStream_t st)
+void launch_typed(const ScanParams& p, int dtype, bool out, bool ends, int64_t blocks, hipStream_t st)
 {
     switch (dtype) {
-    case DCONV_DTYPE_F16: return launch_waves<_Float16>(p, W, out, ends, blocks, st);
-    case DCONV_DTYPE_BF16: return launch_waves<__bf16>(p, W, out, ends, blocks, st);
-    default: return launch_waves<float>(p, W, out, ends, blocks, st);
+    case DCONV_DTYPE_F16: return launch_states<_Float16>(p, out, ends, blocks, st);
+    case DCONV_DTYPE_BF16: return launch_states<__bf16>(p, out, ends, blocks, st);
+    default: return launch_states<float>(p, out, ends, blocks, st);
     }
 }
 
@@ -212,7 +255,8 @@ Rows rows_of(const dconv_tokens& t) { return Rows{t.p, t.sn, t.sl}; }
 
 }  // namespace
 
-int scan_waves(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : S <= 16 ? 4 : 8; }
+int scan_waves(int S) { return S <= 16 ? 4 : 8; }
+int scan_wave_states(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : 4; }
 
 bool scan_sizes_ok(const dconv_scan_args& a)
 {
@@ -229,19 +273,20 @@ ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
 {
     ScanPlan pl;
     pl.waves = scan_waves(a.S);
+    pl.states = scan_wave_states(a.S);
     pl.group = a.C / a.G;
     pl.gblocks = (pl.group - 1) / kWave + 1;
     pl.blocks = a.G * pl.gblocks;
     pl.tiles = (a.L + kT - 1) / kT;
     // Chunks cost another launch that does most of the work again, so there are none where the channels alone give the
-    // chip nearly two waves a SIMD, nor for a few tiles.  Otherwise as many as give it eight (gradients, whose registers let two
-    // be there at a time: four) in chunks of four tiles or more, or half of that in chunks of two.  Measured, S = 16,
-    // us for 1 chunk and those of the rule (sequences x tokens x channels):
-    //   scan      1 x 256 x 2048  41, 26    1 x 4096 x 4096   531, 131    4 x 2048 x 4096  274, 224    8 x 2048 x 4096   352, (407)
-    //   gradient  1 x 256 x 2048 134, 75    1 x 4096 x 4096  1463, 449    4 x 2048 x 4096  928, 799    8 x 2048 x 4096  1261, (1402)
+    // chip one and a half waves a SIMD (gradients: nearly two), nor for a few tiles.  Otherwise as many as give it eight
+    // (gradients, whose registers let two be there at a time: four) in chunks of four tiles or more, or half of that in chunks
+    // of two.  Measured with 16 states, us for 1 chunk and for the rule's (sequences x tokens x channels):
+    //   scan      1 x 256 x 2048   32, 25   1 x 4096 x 4096   431, 135   3 x 2048 x 4096  221, 181   8 x 2048 x 4096   325, (404)
+    //   gradient  1 x 256 x 2048  104, 56   1 x 4096 x 4096  1267, 418   4 x 2048 x 4096  818, 740   8 x 2048 x 4096  1179, (1310)
     const double alone = (double)a.N * pl.blocks * pl.waves;
     pl.chunks = 1;
-    if (alone < 1792 && pl.tiles >= 6) {
+    if (alone < (grad ? 1792 : 1536) && pl.tiles >= (grad ? 6 : 10)) {
         const int most = grad ? (int)(4096 / alone) : (int)(8192 / alone);
         const int longer = most < pl.tiles / 4 ? most : pl.tiles / 4, shorter = most / 2 < pl.tiles / 2 ? most / 2 : pl.tiles / 2;
         pl.chunks = longer > shorter ? longer : shorter;
@@ -259,13 +304,13 @@ int64_t scan_bc_floats(const dconv_scan_args& a, const ScanPlan& pl)
 
 int64_t scan_chunk_floats(const dconv_scan_args& a, const ScanPlan& pl)
 {
-    return pl.chunks > 1 ? (int64_t)a.N * pl.chunks * pl.blocks * kWave * (pl.waves * kR + 1) : 0;
+    return pl.chunks > 1 ? (int64_t)a.N * pl.chunks * pl.blocks * kWave * (pl.waves * pl.states + 1) : 0;
 }
 
 int64_t scan_starts_floats(const dconv_scan_args& a)
 {
     const ScanPlan pl = scan_plan(a, false);
-    return (int64_t)a.N * pl.tiles * pl.blocks * pl.waves * kWave * kR;
+    return (int64_t)a.N * pl.tiles * pl.blocks * pl.waves * kWave * pl.states;
 }
 
 ScanParams scan_params(const dconv_scan_args& a, const ScanPlan& pl)
@@ -290,7 +335,7 @@ int launch_scan_bc(const dconv_scan_args& a, const ScanPlan& pl, float* bc, hipS
     begin_launch();
     auto go = [&](auto* kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, rows_of(a.B), rows_of(a.Cm), a.B.sg, a.Cm.sg, a.lengths, bc,
-                           a.N, a.L, a.G, a.S, pl.waves, pl.tiles);
+                           a.N, a.L, a.G, a.S, pl.waves, pl.states, pl.tiles);
     };
     if (a.dtype == DCONV_DTYPE_F16) go(&bc_kernel<_Float16>);
     else if (a.dtype == DCONV_DTYPE_BF16) go(&bc_kernel<__bf16>);
@@ -302,8 +347,8 @@ int launch_scan_forward(const dconv_scan_args& a, ScanParams p, const ScanPlan& 
 {
     begin_launch();
     if (pl.chunks > 1)                                        // (the last chunk's end is nobody's start)
-        launch_typed(p, a.dtype, pl.waves, false, true, p.total - (int64_t)a.N * pl.blocks, st);
-    launch_typed(p, a.dtype, pl.waves, out, false, p.total, st);
+        launch_typed(p, a.dtype, false, true, p.total - (int64_t)a.N * pl.blocks, st);
+    launch_typed(p, a.dtype, out, false, p.total, st);
     return launch_status();
 }
 
@@ -360,7 +405,7 @@ int dconv_scan(const dconv_scan_args* a, void* stream)
     float* ws = (float*)a->workspace;
     p.bc = ws;
     p.ends = ws + scan_bc_floats(*a, pl);
-    p.dsum = p.ends + (int64_t)a->N * pl.chunks * pl.blocks * pl.waves * kWave * kR;
+    p.dsum = p.ends + (int64_t)a->N * pl.chunks * pl.blocks * pl.waves * kWave * pl.states;
     const int rb = launch_scan_bc(*a, pl, ws, (hipStream_t)stream);
     return rb != DCONV_OK ? rb : launch_scan_forward(*a, p, pl, a->out.p != nullptr, (hipStream_t)stream);
 }

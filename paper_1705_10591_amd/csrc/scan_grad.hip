@@ -12,7 +12,7 @@
 // more instructions than all the rest (6 each).  Pairs of values are added over half of the lanes instead, one value left in
 // either half (two instructions a pair with the swaps of 32 and 16 lanes), so that the number of values halves with the
 // lanes they still have to be added over: 2.2 instructions a value, and at the end lane l of a wave has the sum of
-// value l of 64 (8 tokens, 4 states, B and C).  Channel blocks meet in a second kernel, in the same order on every call.
+// value l of 64 (B and C of 8 tokens and 4 states, say).  Channel blocks meet in a second kernel, in the same order on every call.
 #include "scan_kernel.h"
 
 namespace dconv {
@@ -43,22 +43,25 @@ template <int CTRL> __device__ __forceinline__ float fold(float a, float b, bool
     return keep + value(__builtin_amdgcn_update_dpp(0, bits(give), CTRL, 0xf, 0xf, true));
 }
 
+// Tokens whose sums over lanes make a register: 64 values of 4 states, 64 of 2, 32 of 1 (twice each).
+__host__ __device__ constexpr int gathered(int R) { return R == 4 ? 8 : 16; }
+
 constexpr int kAcross8 = 0x128, kAcross4 = 0x141, kAcross2 = 0x4e, kAcross1 = 0xb1;   // lane bits 3, 2, 1, 0
 
 // What each chunk but the first leaves of g at its start, begun at zero (the last: at the gradient of the call's last
 // state), and its sum of d.
-template <typename T, int W, bool WHOLE>
+template <typename T, int W, int R, bool WHOLE>
 __device__ __forceinline__ void back_block(const ScanParams& p, const ScanPlace& a, float2 (&step)[kT][kWave])   // d, dy
 {
     constexpr int E = kT / W;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c = a.c0 + lane, s0 = wave * kR;
+    const int c = a.c0 + lane, s0 = wave * R;
     const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
-    float A[kR], carry[kR] = {}, dtotal = 0.f, dbias[E] = {};
+    float A[R], carry[R] = {}, dtotal = 0.f, dbias[E] = {};
     const bool ok = WHOLE || lane < a.nc;
     load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
 #pragma unroll
-    for (int r = 0; r < kR; ++r) A[r] *= kLog2e;
+    for (int r = 0; r < R; ++r) A[r] *= kLog2e;
     if (a.chunk == p.chunks - 1 && p.dstate_out)
         load_states(p.dstate_out + ((int64_t)a.n * p.C + c) * p.S, s0, p.S, ok, carry);
     if (nv > 0 && p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
@@ -74,10 +77,10 @@ __device__ __forceinline__ void back_block(const ScanParams& p, const ScanPlace&
         }
         pd.back(); pg.back(); pz.back();
     };
-    BC bc, next;
+    BC<true> bc, next;
     if (a.stop > a.tile0) {
         fetch(t);
-        bc.load(bc_of(p, a, a.stop - 1, W, wave) + (kT - kStep) / 2);
+        bc.load(bc_of(p, a, a.stop - 1, W, wave) + kT - kStep);
     }
     for (int tile = a.stop - 1; tile >= a.tile0; --tile, t -= kT) {
         float raw[E], d_[E], dy[E];
@@ -107,7 +110,7 @@ __device__ __forceinline__ void back_block(const ScanParams& p, const ScanPlace&
         const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, max(tile - 1, a.tile0), W, wave);
 #pragma unroll
         for (int k0 = kT - kStep; k0 >= 0; k0 -= kStep) {
-            next.load(k0 ? here + (k0 - kStep) / 2 : after + (kT - kStep) / 2);
+            next.load(k0 ? here + k0 - kStep : after + kT - kStep);
 #pragma unroll
             for (int k = 0; k < kStep; ++k)
                 if (k0) dn[k] = step[k0 - kStep + k][lane];
@@ -115,7 +118,7 @@ __device__ __forceinline__ void back_block(const ScanParams& p, const ScanPlace&
 #pragma unroll
             for (int k = kStep - 1; k >= 0; --k) {
 #pragma unroll
-                for (int r = 0; r < kR; ++r) carry[r] = exp2_(d[k].x * A[r]) * __builtin_fmaf(bc.c(k, r), d[k].y, carry[r]);
+                for (int r = 0; r < R; ++r) carry[r] = exp2_(d[k].x * A[r]) * __builtin_fmaf(bc.c(k, r), d[k].y, carry[r]);
                 dtotal += d[k].x;
             }
             in_order();
@@ -126,11 +129,11 @@ __device__ __forceinline__ void back_block(const ScanParams& p, const ScanPlace&
         meet();
     }
     const int64_t row = (int64_t)a.n * p.chunks + a.chunk;
-    store_states(p.back + lane_states(p, a, row, W, wave, lane), carry);
+    store_states(p.back + lane_states<W, R>(p, a, row, wave, lane), carry);
     if (wave == 0) p.dsum[(row * p.blocks + a.block) * kWave + lane] = dtotal;
 }
 
-template <typename T, int W>
+template <typename T, int W, int R>
 __global__ void __launch_bounds__(kWave * W)
 scan_back_kernel(ScanParams p)
 {
@@ -140,8 +143,8 @@ scan_back_kernel(ScanParams p)
     a.tile0 += p.chunk_tiles;
     a.tile1 = min(a.tile0 + p.chunk_tiles, p.tiles);
     a.stop = max(a.tile0, min(a.tile1, (a.len + kT - 1) / kT));
-    if (a.nc == kWave) back_block<T, W, true>(p, a, step);
-    else back_block<T, W, false>(p, a, step);
+    if (a.nc == kWave) back_block<T, W, R, true>(p, a, step);
+    else back_block<T, W, R, false>(p, a, step);
 }
 
 template <int W> struct GradLds {
@@ -150,30 +153,31 @@ template <int W> struct GradLds {
     float sums[3][W][kT][kWave];                        // over a wave's states: C h, g B, e A
 };
 
-template <typename T, int W, bool WHOLE>
+template <typename T, int W, int R, bool WHOLE>
 __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace& a, GradLds<W>& lds)
 {
     constexpr int E = kT / W;
+    constexpr int kGather = gathered(R);
     auto& step = lds.step;
     auto& gout = lds.gout;
     auto& sums = lds.sums;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c = a.c0 + lane, s0 = wave * kR;
+    const int c = a.c0 + lane, s0 = wave * R;
     const bool ok = WHOLE || lane < a.nc, gate = p.z.p != nullptr;
     const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
 
-    float A[kR], carry[kR] = {}, dA[kR] = {};
+    float A[R], carry[R] = {}, dA[R] = {};
     load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
     const int64_t own = ((int64_t)a.n * p.C + c) * p.S, row = (int64_t)a.n * p.chunks;
     if (a.chunk == p.chunks - 1) {
         if (p.dstate_out) load_states(p.dstate_out + own, s0, p.S, ok, carry);
     } else {
         for (int k = p.chunks - 1; k > a.chunk; --k) {
-            float e[kR];
-            load_states(p.back + lane_states(p, a, row + k, W, wave, lane), e);
+            float e[R];
+            load_states(p.back + lane_states<W, R>(p, a, row + k, wave, lane), e);
             const float d = p.dsum[((row + k) * p.blocks + a.block) * kWave + lane];
 #pragma unroll
-            for (int r = 0; r < kR; ++r) carry[r] = __builtin_fmaf(exp2_(d * (A[r] * kLog2e)), carry[r], e[r]);
+            for (int r = 0; r < R; ++r) carry[r] = __builtin_fmaf(exp2_(d * (A[r] * kLog2e)), carry[r], e[r]);
         }
     }
     float dbias[E] = {}, skip[E] = {}, sumD[E] = {}, sumB[E] = {};
@@ -195,9 +199,9 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
     Share<const T, E> pu(p.u, a.n, t, ec), pd(p.delta, a.n, t, ec), pg(p.dout, a.n, t, ec), pz(p.z, a.n, t, ec);
     // what a tile reads, asked for a tile ahead
     Run<T, E> un{}, dln{}, gon{}, zn{};
-    float hn[kR] = {};
+    float hn[R] = {};
     auto fetch = [&](int tile, int at) {
-        load_states(p.starts + lane_states(p, a, (int64_t)a.n * p.tiles + tile, W, wave, lane), hn);
+        load_states(p.starts + lane_states<W, R>(p, a, (int64_t)a.n * p.tiles + tile, wave, lane), hn);
         if (at < a.len && nv > 0) {
             un = pu.load(nv);
             dln = pd.load(nv);
@@ -206,16 +210,16 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
         }
         pu.back(); pd.back(); pg.back(); pz.back();
     };
-    BC bc, next;
+    BC<true> bc, next;
     if (a.stop > a.tile0) {
         fetch(a.stop - 1, t);
         bc.load(bc_of(p, a, a.stop - 1, W, wave));
     }
     for (int tile = a.stop - 1; tile >= a.tile0; --tile, t -= kT) {
         Run<T, E> u = un, dl = dln, go = gon, z = zn;
-        float h0[kR];
+        float h0[R];
 #pragma unroll
-        for (int r = 0; r < kR; ++r) h0[r] = hn[r];
+        for (int r = 0; r < R; ++r) h0[r] = hn[r];
         float raw[E], d_[E], dy_[E], u_[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) {
@@ -242,14 +246,14 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
         if (tile > a.tile0) fetch(tile - 1, t - kT);
         meet();
         const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, max(tile - 1, a.tile0), W, wave);
-        float dec[kT][kR], h[kT][kR];
+        float dec[kT][R], h[kT][R];
         float2 s[kStep], sn[kStep];
 #pragma unroll
         for (int k = 0; k < kStep; ++k) s[k] = step[k][lane];
 #pragma unroll
         for (int k0 = 0; k0 < kT; k0 += kStep) {
             const bool more = k0 + kStep < kT;
-            if (more) next.load(here + (k0 + kStep) / 2);
+            if (more) next.load(here + k0 + kStep);
 #pragma unroll
             for (int k = 0; k < kStep; ++k)
                 if (more) sn[k] = step[k0 + kStep + k][lane];
@@ -258,12 +262,12 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
             for (int k = k0; k < k0 + kStep; ++k) {
                 float y = 0.f;
 #pragma unroll
-                for (int r = 0; r < kR; ++r) {
+                for (int r = 0; r < R; ++r) {
                     dec[k][r] = exp2_(s[k - k0].x * (A[r] * kLog2e));
                     h[k][r] = __builtin_fmaf(dec[k][r], k ? h[k - 1][r] : h0[r], s[k - k0].y * bc.b(k - k0, r));
                     y = r ? __builtin_fmaf(bc.c(k - k0, r), h[k][r], y) : bc.c(k - k0, r) * h[k][r];
                 }
-                if (gate) sums[0][wave][k][lane] = y;
+                sums[0][wave][k][lane] = y;
             }
             in_order();
             if (more) {
@@ -272,12 +276,12 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
                 for (int k = 0; k < kStep; ++k) s[k] = sn[k];
             }
         }
-        float packed[8], dy[kStep], dyn[kStep];
+        float packed[kGather], dy[kStep], dyn[kStep];
 #pragma unroll
         for (int k = 0; k < kStep; ++k) dy[k] = gout[kT - kStep + k][lane];
 #pragma unroll
         for (int k0 = kT - kStep; k0 >= 0; k0 -= kStep) {
-            next.load(k0 ? here + (k0 - kStep) / 2 : after);
+            next.load(k0 ? here + k0 - kStep : after);
 #pragma unroll
             for (int k = 0; k < kStep; ++k) {
                 if (!k0) continue;
@@ -288,9 +292,9 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
 #pragma unroll
             for (int k = k0 + kStep - 1; k >= k0; --k) {
                 const int j = k - k0;
-                float q = 0.f, ea = 0.f, pair[kR];
+                float q = 0.f, ea = 0.f, pair[R];
 #pragma unroll
-                for (int r = 0; r < kR; ++r) {
+                for (int r = 0; r < R; ++r) {
                     const float g = __builtin_fmaf(bc.c(j, r), dy[j], carry[r]);
                     carry[r] = g * dec[k][r];
                     const float e = carry[r] * (k ? h[k - 1][r] : h0[r]);
@@ -301,14 +305,21 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
                 }
                 sums[1][wave][k][lane] = q;
                 sums[2][wave][k][lane] = ea;
-                packed[k & 7] = fold<kAcross8>(fold16(pair[0], pair[2]), fold16(pair[1], pair[3]), lane & 8);
-                if ((k & 7) == 0) {
-                    float f[4], e[2];
+                // lane bit 5: B or C; bits 4 and 3 the state, the rest the token, as far as there are states
+                if constexpr (R == 4) packed[k & 7] = fold<kAcross8>(fold16(pair[0], pair[2]), fold16(pair[1], pair[3]), lane & 8);
+                else packed[k] = fold16(pair[0], pair[R - 1]);
+                if (k % kGather == 0) {
+                    float f[4], e[2], g[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) f[i] = fold<kAcross4>(packed[i], packed[i + 4], lane & 4);
+                    for (int i = 0; i < 8; ++i) {
+                        if constexpr (R == 4) g[i] = packed[i];
+                        else g[i] = fold<kAcross8>(packed[i], packed[i + 8], lane & 8);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f[i] = fold<kAcross4>(g[i], g[i + 4], lane & 4);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) e[i] = fold<kAcross2>(f[i], f[i + 2], lane & 2);
-                    const int64_t at = (((int64_t)a.block * p.N + a.n) * p.tiles + tile) * 2 + k / 8;
+                    const int64_t at = (((int64_t)a.block * p.N + a.n) * p.tiles + tile) * (kT / kGather) + k / kGather;
                     p.part_bc[(at * W + wave) * kWave + lane] = fold<kAcross1>(e[0], e[1], lane & 1);
                 }
             }
@@ -322,22 +333,30 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
         }
         meet();
         if (nv > 0 && t < p.L) {
-            float du[E], dd[E], dz[E];
+            float du[E], dd[E], dz[E], y[E], q[E] = {}, ea[E] = {}, dy[E];
+            const Run<float, E> dyr = lds_run<E>(&gout[tt][tc]);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const float2 s = step[tt][tc + i];
-                const float dy = gout[tt][tc + i], ui = u[i];
-                float y = skip[i] * ui, q = 0.f, ea = 0.f;
+                y[i] = skip[i] * u[i];
+                dy[i] = dyr[i];
+            }
 #pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    if (gate) y += sums[0][w][tt][tc + i];
-                    q += sums[1][w][tt][tc + i];
-                    ea += sums[2][w][tt][tc + i];
+            for (int w = 0; w < W; ++w) {
+                const Run<float, E> r0 = lds_run<E>(&sums[0][w][tt][tc]), r1 = lds_run<E>(&sums[1][w][tt][tc]),
+                                    r2 = lds_run<E>(&sums[2][w][tt][tc]);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    y[i] += r0[i];
+                    q[i] += r1[i];
+                    ea[i] += r2[i];
                 }
-                du[i] = __builtin_fmaf(s.x, q, skip[i] * dy);
-                dd[i] = __builtin_fmaf(ui, q, ea);
-                dz[i] = y;
-                sumD[i] = __builtin_fmaf(dy, t < a.len ? ui : 0.f, sumD[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                du[i] = __builtin_fmaf(step[tt][tc + i].x, q[i], skip[i] * dy[i]);
+                dd[i] = __builtin_fmaf(u[i], q[i], ea[i]);
+                dz[i] = y[i];
+                sumD[i] = __builtin_fmaf(dy[i], t < a.len ? u[i] : 0.f, sumD[i]);
             }
             if (p.softplus) {
 #pragma unroll
@@ -364,8 +383,8 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
         }
         qu.back(); qd.back(); qz.back();
     }
-    if (a.chunk == 0 && p.dstate && ok) store_some<kR>(p.dstate + own + s0, p.S - s0, carry);
-    store_states(p.part_A + lane_states(p, a, row + a.chunk, W, wave, lane), dA);
+    if (a.chunk == 0 && p.dstate && ok) store_some<R>(p.dstate + own + s0, p.S - s0, carry);
+    store_states(p.part_A + lane_states<W, R>(p, a, row + a.chunk, wave, lane), dA);
     // dD and the gradient of the bias: over the sixteen tokens of a tile
     __syncthreads();
 #pragma unroll
@@ -384,30 +403,32 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
     }
 }
 
-template <typename T, int W>
+template <typename T, int W, int R>
 __global__ void __launch_bounds__(kWave * W, 2)
 scan_grad_kernel(ScanParams p)
 {
     __shared__ GradLds<W> lds;
     const ScanPlace a = scan_place(p);
-    if (a.nc == kWave) grad_block<T, W, true>(p, a, lds);
-    else grad_block<T, W, false>(p, a, lds);
+    if (a.nc == kWave) grad_block<T, W, R, true>(p, a, lds);
+    else grad_block<T, W, R, false>(p, a, lds);
 }
 
-// dB and dC of 64 values (8 tokens, 4 states) from the parts of a group's channel blocks.
+// dB and dC from the parts of a group's channel blocks; lane l of a unit has the value that lane l had above.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 scan_sum_bc_kernel(const float* part, Rows dB, Rows dC, int64_t b_g, int64_t c_g, const int* lengths, int N, int L, int G, int S,
-                   int W, int tiles, int gblocks)
+                   int W, int R, int tiles, int gblocks)
 {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const int lane = (int)(i & 63);
-    const int64_t unit = i >> 6, per = (int64_t)tiles * 2 * W;             // a wave's share: [G][N][tiles][2][W]
+    const int tokens = gathered(R);
+    const int64_t unit = i >> 6, per = (int64_t)tiles * (kT / tokens) * W;      // units [G][N][tiles][kT / tokens][W]
     const int64_t seq = unit / per, in = unit - seq * per;
     const int g = (int)(seq / N), n = (int)(seq - (int64_t)g * N);
     if (g >= G) return;
-    const int w = (int)(in % W);
-    const int t = (int)(in / W) * 8 + (lane & 7), s = w * kR + (lane >> 4 & 1) * 2 + (lane >> 3 & 1);
+    const int w = (int)(in % W), t = (int)(in / W) * tokens + (lane & (tokens - 1));
+    const int r = R == 4 ? (lane >> 4 & 1) * 2 + (lane >> 3 & 1) : lane >> 4 & 1, s = w * R + r;
+    if (r >= R) return;
     if (t >= L || s >= S) return;
     float v = 0.f;
     if (t < length_of(lengths, n, L))
@@ -416,52 +437,51 @@ scan_sum_bc_kernel(const float* part, Rows dB, Rows dC, int64_t b_g, int64_t c_g
     else dC.at<T>(n, t, 0)[g * c_g + s] = (T)v;
 }
 
-// dA, dD and the gradient of the bias from the parts of all sequences and chunks.
-__global__ void __launch_bounds__(kWave)
-scan_sum_kernel(ScanParams p, int W, float* dA, float* dD, float* dbias)
+// dA, dD and the gradient of the bias from the parts of all sequences and chunks: four waves take a quarter of them each.
+__global__ void __launch_bounds__(kThreads)
+scan_sum_kernel(ScanParams p, int W, int R, float* dA, float* dD, float* dbias)
 {
-    const int lane = threadIdx.x, block = blockIdx.x / (W + 1), w = blockIdx.x - block * (W + 1);
-    const int g = block / p.gblocks, k = block - g * p.gblocks, c = g * p.group + k * kWave + lane;
-    const bool ok = k * kWave + lane < p.group;
+    __shared__ float red[4][kWave];
+    const int values = W * R + 2, block = blockIdx.x / values, v = blockIdx.x - block * values;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t rows = (int64_t)p.N * p.chunks;
-    if (w < W) {
-        float s[kR] = {};
-        for (int64_t r = 0; r < rows; ++r) {
-            float v[kR];
-            load_states(p.part_A + (((r * p.blocks + block) * W + w) * kWave + lane) * kR, v);
-            for (int i = 0; i < kR; ++i) s[i] += v[i];
-        }
-        if (ok) store_some<kR>(dA + (int64_t)c * p.S + w * kR, p.S - w * kR, s);
-        return;
+    const float* from = v < W * R ? p.part_A + ((int64_t)block * W * kWave + v / R * kWave + lane) * R + v % R
+                                  : (v == W * R ? p.part_D : p.part_bias) + (int64_t)block * kWave + lane;
+    const int64_t step = (int64_t)p.blocks * kWave * (v < W * R ? W * R : 1);
+    float s = 0.f;
+#pragma unroll 4
+    for (int64_t r = wave; r < rows; r += 4) s += from[r * step];
+    red[wave][lane] = s;
+    __syncthreads();
+    const int g = block / p.gblocks, k = block - g * p.gblocks, c = g * p.group + k * kWave + lane;
+    if (wave || k * kWave + lane >= p.group) return;
+    s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    if (v < W * R) {
+        if (v < p.S) dA[(int64_t)c * p.S + v] = s;
+    } else if (v == W * R) {
+        if (dD) dD[c] = s;
+    } else if (dbias) {
+        dbias[c] = s;
     }
-    float d = 0.f, b = 0.f;
-    for (int64_t r = 0; r < rows; ++r) {
-        d += p.part_D[(r * p.blocks + block) * kWave + lane];
-        b += p.part_bias[(r * p.blocks + block) * kWave + lane];
-    }
-    if (ok && dD) dD[c] = d;
-    if (ok && dbias) dbias[c] = b;
 }
 
-template <typename T, int W> void launch_kernels(const ScanParams& p, hipStream_t st)
+template <typename T, int W, int R> void launch_kernels(const ScanParams& p, hipStream_t st)
 {
     if (p.chunks > 1)
-        hipLaunchKernelGGL((scan_back_kernel<T, W>), dim3((unsigned)(p.total - (int64_t)p.N * p.blocks)), dim3(kWave * W), 0, st, p);
-    hipLaunchKernelGGL((scan_grad_kernel<T, W>), dim3((unsigned)p.total), dim3(kWave * W), 0, st, p);
+        hipLaunchKernelGGL((scan_back_kernel<T, W, R>), dim3((unsigned)(p.total - (int64_t)p.N * p.blocks)), dim3(kWave * W), 0, st, p);
+    hipLaunchKernelGGL((scan_grad_kernel<T, W, R>), dim3((unsigned)p.total), dim3(kWave * W), 0, st, p);
 }
 
-template <typename T> void launch_typed(const dconv_scan_args& a, const ScanParams& p, int W, hipStream_t st)
+template <typename T> void launch_typed(const dconv_scan_args& a, const ScanParams& p, int W, int R, hipStream_t st)
 {
-    switch (W) {
-    case 1: launch_kernels<T, 1>(p, st); break;
-    case 2: launch_kernels<T, 2>(p, st); break;
-    case 4: launch_kernels<T, 4>(p, st); break;
-    default: launch_kernels<T, 8>(p, st); break;
-    }
-    const int64_t n = (int64_t)p.N * p.G * p.tiles * 2 * W * kWave;
+    if (a.S <= 4) launch_kernels<T, 4, 1>(p, st);
+    else if (a.S <= 8) launch_kernels<T, 4, 2>(p, st);
+    else if (a.S <= 16) launch_kernels<T, 4, 4>(p, st);
+    else launch_kernels<T, 8, 4>(p, st);
+    const int64_t n = (int64_t)p.N * p.G * p.tiles * (kT / gathered(R)) * W * kWave;
     hipLaunchKernelGGL((scan_sum_bc_kernel<T>), dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p.part_bc,
                        Rows{a.dB.p, a.dB.sn, a.dB.sl}, Rows{a.dC.p, a.dC.sn, a.dC.sl}, a.dB.sg, a.dC.sg, a.lengths, a.N, a.L,
-                       a.G, a.S, W, p.tiles, p.gblocks);
+                       a.G, a.S, W, R, p.tiles, p.gblocks);
 }
 
 // The workspace of a gradient call, in floats: where its parts begin, and how many there are.
@@ -469,17 +489,17 @@ struct GradSpace { int64_t ends, end_sums, back, dsum, bc_parts, A_parts, D_part
 
 GradSpace space_of(const dconv_scan_args& a, const ScanPlan& pl)
 {
-    const int64_t rows = (int64_t)a.N * pl.chunks * pl.blocks * kWave, states = rows * pl.waves * kR;
+    const int64_t rows = (int64_t)a.N * pl.chunks * pl.blocks * kWave, states = rows * pl.waves * pl.states;
     const ScanPlan fw = scan_plan(a, false);             // of the launches that make the states again
     const int64_t frows = a.starts || fw.chunks < 2 ? 0 : (int64_t)a.N * fw.chunks * fw.blocks * kWave;
     GradSpace s;
     int64_t at = scan_bc_floats(a, pl);
     auto take = [&](int64_t n) { const int64_t here = at; at += (n + 3) / 4 * 4; return here; };
-    s.ends = take(frows * fw.waves * kR);
+    s.ends = take(frows * fw.waves * fw.states);
     s.end_sums = take(frows);
     s.back = take(pl.chunks > 1 ? states : 0);
     s.dsum = take(pl.chunks > 1 ? rows : 0);
-    s.bc_parts = take((int64_t)pl.blocks * a.N * pl.tiles * 2 * pl.waves * kWave);
+    s.bc_parts = take((int64_t)pl.blocks * a.N * pl.tiles * (kT / gathered(pl.states)) * pl.waves * kWave);
     s.A_parts = take(states);
     s.D_parts = take(rows);
     s.bias_parts = take(rows);
@@ -528,10 +548,10 @@ int dconv_scan_grad(const dconv_scan_args* a, void* stream)
         if (rc != DCONV_OK) return rc;
     }
     begin_launch();
-    if (a->dtype == DCONV_DTYPE_F16) launch_typed<_Float16>(*a, p, pl.waves, st);
-    else if (a->dtype == DCONV_DTYPE_BF16) launch_typed<__bf16>(*a, p, pl.waves, st);
-    else launch_typed<float>(*a, p, pl.waves, st);
-    hipLaunchKernelGGL(scan_sum_kernel, dim3((unsigned)(pl.blocks * (pl.waves + 1))), dim3(kWave), 0, st, p, pl.waves, a->dA, a->dD,
+    if (a->dtype == DCONV_DTYPE_F16) launch_typed<_Float16>(*a, p, pl.waves, pl.states, st);
+    else if (a->dtype == DCONV_DTYPE_BF16) launch_typed<__bf16>(*a, p, pl.waves, pl.states, st);
+    else launch_typed<float>(*a, p, pl.waves, pl.states, st);
+    hipLaunchKernelGGL(scan_sum_kernel, dim3((unsigned)(pl.blocks * (pl.waves * pl.states + 2))), dim3(kThreads), 0, st, p, pl.waves, pl.states, a->dA, a->dD,
                        a->ddelta_bias);
     return launch_status();
 }

@@ -2,13 +2,14 @@
 //
 // The recurrence is elementwise, so the work goes to the vector ALU: a product, an exponential, a product and two
 // multiply-adds for each (token, channel, state).  What shapes the kernels:
-//  * A lane is a channel and a wave has kR = 4 states of 64 channels: B[t] and C[t] are then the same for a whole wave and
-//    come through scalar registers, which costs the vector ALU nothing.  The W = S / 4 waves of a workgroup have the other
-//    states of the same channels; what all states of a channel share (d, d u, the sum over states) goes through LDS.
+//  * A lane is a channel and a wave has R states of 64 channels: B[t] and C[t] are then the same for a whole wave and come
+//    through scalar registers, which costs the vector ALU nothing.  The W waves of a workgroup have the other states of the
+//    same channels (four waves of 1, 2 or 4 states, or eight of 4); what all states of a channel share (d, d u, the sum
+//    over states) goes through LDS.
 //  * Tokens come in tiles of kT = 16.  Thread by thread a tile's 16 x 64 values are loaded and stored in runs of E = 16 / W
 //    channels, and d, its softplus and the gate are computed once, not once per wave.
-//  * bc_kernel lays B and C out for the scalar loads first: fp32, [N][G][tiles][W][16 tokens][4 of B, 4 of C], zeros behind
-//    the end of a sequence and beyond state S.  With d = 0 there too, tokens that do not count leave the state as it is,
+//  * bc_kernel lays B and C out for the scalar loads first: fp32, [N][G][tiles][W][8 pairs of tokens][4 + 4 of B, 4 + 4 of C], R of each 4
+//    used, zeros behind the end of a sequence and beyond state S.  With d = 0 there too, tokens that do not count leave the state as it is,
 //    and the loops need no masks.
 //  * Scalar loads come back in any order, so that a wait for one is a wait for all: a tile is walked in steps of kStep = 4
 //    tokens, and the operands of the next step (64 of B and C in scalar registers, d and d u from LDS) are asked for before the
@@ -22,24 +23,26 @@
 namespace dconv {
 
 constexpr int kT = 16;               // tokens of a tile
-constexpr int kR = 4;                // states of a wave
+constexpr int kR = 4;                // states of a wave, at most
 constexpr int kStep = 4;             // tokens whose operands are fetched together
 constexpr int kMaxStates = 32;       // eight waves
 
-typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef float f16 __attribute__((ext_vector_type(16), aligned(16)));
-typedef const __attribute__((address_space(4))) f16* bc_ptr;       // constant memory: scalar loads, two tokens each
+typedef float f8 __attribute__((ext_vector_type(8), aligned(16)));
+typedef const __attribute__((address_space(4))) f8* bc_ptr;        // constant memory: scalar loads
 
-// B and C of kStep tokens.
-struct BC {
-    f16 v[kStep / 2];
+// B of kStep tokens, and C where it is needed (WITH_C): pairs of tokens, four states each.
+template <bool WITH_C> struct BC {
+    f8 vb[kStep / 2], vc[WITH_C ? kStep / 2 : 1];
     __device__ __forceinline__ void load(bc_ptr p)
     {
 #pragma unroll
-        for (int i = 0; i < kStep / 2; ++i) v[i] = p[i];
+        for (int i = 0; i < kStep / 2; ++i) {
+            vb[i] = p[2 * i];
+            if (WITH_C) vc[i] = p[2 * i + 1];
+        }
     }
-    __device__ __forceinline__ float b(int k, int r) const { return v[k / 2][k % 2 * 8 + r]; }
-    __device__ __forceinline__ float c(int k, int r) const { return v[k / 2][k % 2 * 8 + kR + r]; }
+    __device__ __forceinline__ float b(int k, int r) const { return vb[k / 2][k % 2 * kR + r]; }
+    __device__ __forceinline__ float c(int k, int r) const { return vc[k / 2][k % 2 * kR + r]; }
 };
 
 struct Rows {                        // a token tensor: base, elements between sequences and tokens
@@ -57,10 +60,10 @@ struct ScanParams {
     float *state_out, *dstate, *starts;
     const int* lengths;
     const float* bc;
-    float *ends, *dsum;              // of the chunks: states [N][chunks][blocks][W][64][4], sums of d [N][chunks][blocks][64]
+    float *ends, *dsum;              // of the chunks: states [N][chunks][blocks][W][64][R], sums of d [N][chunks][blocks][64]
     float *back;                     // ... and of the way back, laid out like ends
-    float *part_bc;                  // gradients of B and C: [blocks][N][tiles][2][W][64]
-    float *part_A, *part_D, *part_bias;   // [N][chunks][blocks][W][64][4], [N][chunks][blocks][64]
+    float *part_bc;                  // gradients of B and C: [blocks][N][tiles][2][W][64], see scan_grad.hip
+    float *part_A, *part_D, *part_bias;   // [N][chunks][blocks][W][64][R], [N][chunks][blocks][64]
     int N, L, C, S, G, softplus;
     int group, gblocks, blocks;      // channels of a group, its blocks of 64, all blocks
     int tiles, chunk_tiles, chunks;  // of L tokens
@@ -91,10 +94,10 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanParams& p)
     return a;
 }
 
-// ... of a wave and tile; a token takes half an f16
+// ... of a wave and tile; a token takes one f8's worth
 __device__ __forceinline__ bc_ptr bc_of(const ScanParams& p, const ScanPlace& a, int tile, int W, int wave)
 {
-    return (bc_ptr)(p.bc) + ((((int64_t)a.n * p.G + a.g) * p.tiles + tile) * W + wave) * (kT / 2);
+    return (bc_ptr)(p.bc) + ((((int64_t)a.n * p.G + a.g) * p.tiles + tile) * W + wave) * kT;
 }
 
 // d of a run of channels, before the tokens that do not count are masked.
@@ -107,6 +110,12 @@ template <int E> __device__ __forceinline__ void steps_of(bool soft, const float
     for (int i = 0; i < E; ++i) d[i] = softplus(raw[i]);
 }
 
+// A run of E values in LDS, whose rows begin at multiples of 16 bytes.
+template <int E> __device__ __forceinline__ Run<float, E> lds_run(const float* p)
+{
+    return load_run<E>((const float*)__builtin_assume_aligned(p, E >= 4 ? 16 : 4 * E));
+}
+
 // Nothing moves past this point: what is written above it is under way before what is written below begins.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
@@ -116,46 +125,47 @@ template <typename T, int E> struct Share {
     T* p;
     int64_t step;
     __device__ __forceinline__ Share(const Rows& rows, int n, int t, int c) : p(rows.at<T>(n, t, c)), step(rows.l * kT) {}
+    // the step in vector registers, where B and C take most of the scalar ones and there are vector ones to spare
+    __device__ __forceinline__ void spare() { asm("" : "+v"(step)); }
     __device__ __forceinline__ void forward() { p += step; }
     __device__ __forceinline__ void back() { p -= step; }
     __device__ __forceinline__ auto load(int nv) const { return load_some<E>(p, nv); }
     __device__ __forceinline__ void store(int nv, const float (&v)[E]) const { store_some<E>(p, nv, v); }
 };
 
-// Index of this lane's four states among those of all channels.
-__device__ __forceinline__ int64_t lane_states(const ScanParams& p, const ScanPlace& a, int64_t row, int W, int wave, int lane)
+// Index of this lane's states among those of all channels.
+template <int W, int R>
+__device__ __forceinline__ int64_t lane_states(const ScanParams& p, const ScanPlace& a, int64_t row, int wave, int lane)
 {
-    return (((row * p.blocks + a.block) * W + wave) * kWave + lane) * kR;
+    return (((row * p.blocks + a.block) * W + wave) * kWave + lane) * R;
 }
 
-// Four states of a channel in a user's [C][S], of which those beyond S are 0.
-__device__ __forceinline__ void load_states(const float* p, int s0, int S, bool ok, float (&v)[kR])
+// The states from s0 on of a channel in a user's [C][S], of which those beyond S are 0.
+template <int R> __device__ __forceinline__ void load_states(const float* p, int s0, int S, bool ok, float (&v)[R])
 {
 #pragma unroll
-    for (int r = 0; r < kR; ++r) v[r] = 0.f;
-    if (ok) load_some<kR>(p + s0, S - s0, v);
+    for (int r = 0; r < R; ++r) v[r] = 0.f;
+    if (ok) load_some<R>(p + s0, S - s0, v);
 }
 
-__device__ __forceinline__ void load_states(const float* p, float (&v)[kR])
+// ... in the library's own arrays
+template <int R> __device__ __forceinline__ void load_states(const float* p, float (&v)[R])
 {
-    const f4 t = *(const f4*)p;
+    const Run<float, R> t = load_run<R>((const float*)__builtin_assume_aligned(p, 4 * R));
 #pragma unroll
-    for (int r = 0; r < kR; ++r) v[r] = t[r];
+    for (int r = 0; r < R; ++r) v[r] = t[r];
 }
-
-__device__ __forceinline__ void store_states(float* p, const float (&v)[kR])
+template <int R> __device__ __forceinline__ void store_states(float* p, const float (&v)[R])
 {
-    f4 t;
-#pragma unroll
-    for (int r = 0; r < kR; ++r) t[r] = v[r];
-    *(f4*)p = t;
+    store_some<R>((float*)__builtin_assume_aligned(p, 4 * R), R, v);
 }
 
 // host side (scan.hip)
-int scan_waves(int S);
+int scan_waves(int S);               // W
+int scan_wave_states(int S);         // R
 bool scan_sizes_ok(const dconv_scan_args& a);
 int scan_check(const dconv_scan_args* a, int form);        // 0 prompt, 1 gradient, 2 step
-struct ScanPlan { int waves, group, gblocks, blocks, tiles, chunks, chunk_tiles; };
+struct ScanPlan { int waves, states, group, gblocks, blocks, tiles, chunks, chunk_tiles; };
 ScanPlan scan_plan(const dconv_scan_args& a, bool grad);
 ScanParams scan_params(const dconv_scan_args& a, const ScanPlan& pl);
 int64_t scan_bc_floats(const dconv_scan_args& a, const ScanPlan& pl);

@@ -88,7 +88,7 @@ extern "C" int dconv_scan_step(const dconv_scan_args* a, void* stream)
     p.b_g = a->B.sg; p.c_g = a->Cm.sg;
     p.A = a->A; p.D = a->D; p.delta_bias = a->delta_bias; p.state = a->state_out; p.slots = a->slots;
     p.M = a->M; p.C = a->C; p.S = a->S; p.group = a->C / a->G; p.softplus = a->softplus;
-    const int W = scan_waves(a->S);
+    const int W = a->S <= 4 ? 1 : a->S <= 8 ? 2 : a->S <= 16 ? 4 : 8;
     p.cblocks = (a->C - 1) / (kThreads / W) + 1;
     const int64_t blocks = (int64_t)a->N * p.cblocks;
     if (blocks > 2147483647LL) return DCONV_BAD_SHAPE;
