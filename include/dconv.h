@@ -484,8 +484,9 @@ long long dconv_causal_workspace(const dconv_causal_args *a);
  * those that dconv_scan left for the same inputs, or NULL: they are made again.
  * dconv_scan_step: L = 1; state_out [M][C][S] is a cache of states, of which row
  * slots[n] is read and updated.  `state` is not used.
- * Decays exp(d * A) are meant to be at most 1 (A <= 0, d >= 0); larger ones are
- * computed as they are, and overflow where the recurrence does.
+ * Decays exp(d * A) are meant to be at most 1 (A <= 0, d >= 0).  Larger ones are
+ * computed as they are; where their product over a sequence passes the largest
+ * fp32 number, results may be infinite or NaN.
  */
 typedef struct dconv_scan_args {
     int dtype, N, L, C, S, G, M, softplus;

@@ -7,6 +7,9 @@
 // States are needed in the order opposite to the one they are made in: they are kept at the start of every tile
 // (`starts`), and a tile of 16 tokens makes its own again in registers, 4 decays and 4 states a token and lane, before it
 // walks back.  About 20 vector instructions for each (token, channel, state) bound the call, not its memory.
+// A call in chunks that is not given starts makes all that they need in one pass (sweep_kernel): the states of each tile
+// as if its chunk began at zero, what the chunk leaves, and what it would leave going back, which is a sum over tokens of
+// C dy times the decays from the chunk's start, products that the pass can carry along.
 //
 // dB and dC are sums over channels, that is over lanes: 2 x 4 values a token.  Adding each over 64 lanes would take
 // more instructions than all the rest (6 each).  Pairs of values are added over half of the lanes instead, one value left in
@@ -147,6 +150,140 @@ scan_back_kernel(ScanParams p)
     else back_block<T, W, R, false>(p, a, step);
 }
 
+// One pass over each chunk from a state of zero (the first: the call's): the state at the start of every tile and what d adds
+// up to until there, the state and sum at the end, and the gradient that the chunk leaves at its start (begun at
+// zero, in the last chunk at the gradient of the call's last state).
+struct SweepLds {
+    float2 step[kT][kWave];                             // d, d u
+    float gout[kT][kWave];                              // dy
+};
+
+template <typename T, int W, int R, bool WHOLE>
+__device__ __forceinline__ void sweep_block(const ScanParams& p, const ScanPlace& a, SweepLds& lds)
+{
+    constexpr int E = kT / W;
+    auto& step = lds.step;
+    auto& gout = lds.gout;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = a.c0 + lane, s0 = wave * R;
+    const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
+    const bool ok = WHOLE || lane < a.nc, gate = p.z.p != nullptr;
+    float A[R], h[R] = {}, q[R] = {}, decay[R], dtotal = 0.f, dbias[E] = {};
+    load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        A[r] *= kLog2e;
+        decay[r] = 1.f;
+    }
+    const int64_t own = ((int64_t)a.n * p.C + c) * p.S, row = (int64_t)a.n * p.chunks + a.chunk;
+    if (a.chunk == 0 && p.state) load_states(p.state + own, s0, p.S, ok, h);
+    if (nv > 0 && p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
+    int t = a.tile0 * kT + tt;
+    Share<const T, E> pu(p.u, a.n, t, ec), pd(p.delta, a.n, t, ec), pg(p.dout, a.n, t, ec), pz(p.z, a.n, t, ec);
+    Run<T, E> u{}, dl{}, go{}, z{};
+    auto fetch = [&](int at) {
+        if (at < a.len && nv > 0) {
+            u = pu.load(nv);
+            dl = pd.load(nv);
+            go = pg.load(nv);
+            if (gate) z = pz.load(nv);
+        }
+        pu.forward(); pd.forward(); pg.forward(); pz.forward();
+    };
+    BC<true> bc, next;
+    if (a.tile0 < a.stop) {
+        fetch(t);
+        bc.load(bc_of(p, a, a.tile0, W, wave));
+    }
+    for (int tile = a.tile0; tile < a.stop; ++tile, t += kT) {
+        float raw[E], d_[E], u_[E], dy_[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            raw[i] = dl[i] + dbias[i];
+            u_[i] = u[i];
+            dy_[i] = go[i];
+        }
+        steps_of(p.softplus, raw, d_);
+        if (gate) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) dy_[i] *= z[i] * sigmoid(z[i]);
+        }
+        if ((tile + 1) * kT > a.len) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if (t >= a.len) d_[i] = u_[i] = dy_[i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            step[tt][tc + i] = make_float2(d_[i], d_[i] * u_[i]);
+            gout[tt][tc + i] = dy_[i];
+        }
+        if (tile + 1 < a.stop) fetch(t + kT);
+        meet();
+        store_states(p.starts + lane_states<W, R>(p, a, (int64_t)a.n * p.tiles + tile, wave, lane), h);
+        if (wave == 0) p.cum[(((int64_t)a.n * p.tiles + tile) * p.blocks + a.block) * kWave + lane] = dtotal;
+        float2 d[kStep], dn[kStep];
+        float dy[kStep], dyn[kStep];
+#pragma unroll
+        for (int k = 0; k < kStep; ++k) {
+            d[k] = step[k][lane];
+            dy[k] = gout[k][lane];
+        }
+        const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, min(tile + 1, a.stop - 1), W, wave);
+#pragma unroll
+        for (int k0 = 0; k0 < kT; k0 += kStep) {
+            const bool more = k0 + kStep < kT;
+            next.load(more ? here + k0 + kStep : after);
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) {
+                if (!more) continue;
+                dn[k] = step[k0 + kStep + k][lane];
+                dyn[k] = gout[k0 + kStep + k][lane];
+            }
+            in_order();
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float e = exp2_(d[k].x * A[r]);
+                    h[r] = __builtin_fmaf(e, h[r], d[k].y * bc.b(k, r));
+                    decay[r] *= e;
+                    q[r] = __builtin_fmaf(decay[r], bc.c(k, r) * dy[k], q[r]);
+                }
+                dtotal += d[k].x;
+            }
+            in_order();
+            bc = next;
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) {
+                d[k] = dn[k];
+                dy[k] = dyn[k];
+            }
+        }
+        meet();
+    }
+    if (a.chunk == p.chunks - 1 && p.dstate_out) {
+        float last[R];
+        load_states(p.dstate_out + own, s0, p.S, ok, last);
+#pragma unroll
+        for (int r = 0; r < R; ++r) q[r] = __builtin_fmaf(decay[r], last[r], q[r]);
+    }
+    store_states(p.ends + lane_states<W, R>(p, a, row, wave, lane), h);
+    store_states(p.back + lane_states<W, R>(p, a, row, wave, lane), q);
+    if (wave == 0) p.dsum[(row * p.blocks + a.block) * kWave + lane] = dtotal;
+}
+
+template <typename T, int W, int R>
+__global__ void __launch_bounds__(kWave * W)
+sweep_kernel(ScanParams p)
+{
+    __shared__ SweepLds lds;
+    const ScanPlace a = scan_place(p);
+    if (a.nc == kWave) sweep_block<T, W, R, true>(p, a, lds);
+    else sweep_block<T, W, R, false>(p, a, lds);
+}
+
 template <int W> struct GradLds {
     float2 step[kT][kWave];                             // d, d u
     float gout[kT][kWave];                              // dy
@@ -180,6 +317,18 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
             for (int r = 0; r < R; ++r) carry[r] = __builtin_fmaf(exp2_(d * (A[r] * kLog2e)), carry[r], e[r]);
         }
     }
+    // the state that the chunk begins at, where its tiles' are as if that were zero
+    float begin[R] = {};
+    const bool later = p.cum && a.chunk;
+    if (later) {
+        for (int k = 0; k < a.chunk; ++k) {
+            float e[R];
+            load_states(p.ends + lane_states<W, R>(p, a, row + k, wave, lane), e);
+            const float d = p.dsum[((row + k) * p.blocks + a.block) * kWave + lane];
+#pragma unroll
+            for (int r = 0; r < R; ++r) begin[r] = __builtin_fmaf(exp2_(d * (A[r] * kLog2e)), begin[r], e[r]);
+        }
+    }
     float dbias[E] = {}, skip[E] = {}, sumD[E] = {}, sumB[E] = {};
     if (nv > 0) {
         if (p.delta_bias) load_some<E>(p.delta_bias + ec, nv, dbias);
@@ -199,9 +348,10 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
     Share<const T, E> pu(p.u, a.n, t, ec), pd(p.delta, a.n, t, ec), pg(p.dout, a.n, t, ec), pz(p.z, a.n, t, ec);
     // what a tile reads, asked for a tile ahead
     Run<T, E> un{}, dln{}, gon{}, zn{};
-    float hn[R] = {};
+    float hn[R] = {}, cumn = 0.f;
     auto fetch = [&](int tile, int at) {
         load_states(p.starts + lane_states<W, R>(p, a, (int64_t)a.n * p.tiles + tile, wave, lane), hn);
+        if (later) cumn = p.cum[(((int64_t)a.n * p.tiles + tile) * p.blocks + a.block) * kWave + lane];
         if (at < a.len && nv > 0) {
             un = pu.load(nv);
             dln = pd.load(nv);
@@ -220,6 +370,10 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
         float h0[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) h0[r] = hn[r];
+        if (later) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) h0[r] = __builtin_fmaf(exp2_(cumn * (A[r] * kLog2e)), begin[r], h0[r]);
+        }
         float raw[E], d_[E], dy_[E], u_[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) {
@@ -467,7 +621,9 @@ scan_sum_kernel(ScanParams p, int W, int R, float* dA, float* dD, float* dbias)
 
 template <typename T, int W, int R> void launch_kernels(const ScanParams& p, hipStream_t st)
 {
-    if (p.chunks > 1)
+    if (p.cum)
+        hipLaunchKernelGGL((sweep_kernel<T, W, R>), dim3((unsigned)p.total), dim3(kWave * W), 0, st, p);
+    else if (p.chunks > 1)
         hipLaunchKernelGGL((scan_back_kernel<T, W, R>), dim3((unsigned)(p.total - (int64_t)p.N * p.blocks)), dim3(kWave * W), 0, st, p);
     hipLaunchKernelGGL((scan_grad_kernel<T, W, R>), dim3((unsigned)p.total), dim3(kWave * W), 0, st, p);
 }
@@ -485,20 +641,19 @@ template <typename T> void launch_typed(const dconv_scan_args& a, const ScanPara
 }
 
 // The workspace of a gradient call, in floats: where its parts begin, and how many there are.
-struct GradSpace { int64_t ends, end_sums, back, dsum, bc_parts, A_parts, D_parts, bias_parts, starts, all; };
+struct GradSpace { int64_t ends, back, dsum, cum, bc_parts, A_parts, D_parts, bias_parts, starts, all; };
 
 GradSpace space_of(const dconv_scan_args& a, const ScanPlan& pl)
 {
     const int64_t rows = (int64_t)a.N * pl.chunks * pl.blocks * kWave, states = rows * pl.waves * pl.states;
-    const ScanPlan fw = scan_plan(a, false);             // of the launches that make the states again
-    const int64_t frows = a.starts || fw.chunks < 2 ? 0 : (int64_t)a.N * fw.chunks * fw.blocks * kWave;
+    const bool chunks = pl.chunks > 1, sweep = chunks && !a.starts;
     GradSpace s;
     int64_t at = scan_bc_floats(a, pl);
     auto take = [&](int64_t n) { const int64_t here = at; at += (n + 3) / 4 * 4; return here; };
-    s.ends = take(frows * fw.waves * fw.states);
-    s.end_sums = take(frows);
-    s.back = take(pl.chunks > 1 ? states : 0);
-    s.dsum = take(pl.chunks > 1 ? rows : 0);
+    s.ends = take(sweep ? states : 0);
+    s.back = take(chunks ? states : 0);
+    s.dsum = take(chunks ? rows : 0);
+    s.cum = take(sweep ? (int64_t)a.N * pl.tiles * pl.blocks * kWave : 0);
     s.bc_parts = take((int64_t)pl.blocks * a.N * pl.tiles * (kT / gathered(pl.states)) * pl.waves * kWave);
     s.A_parts = take(states);
     s.D_parts = take(rows);
@@ -538,14 +693,16 @@ int dconv_scan_grad(const dconv_scan_args* a, void* stream)
     rc = launch_scan_bc(*a, pl, ws, st);
     if (rc != DCONV_OK) return rc;
     if (!a->starts) {
-        const ScanPlan fw = scan_plan(*a, false);
-        ScanParams forward = scan_params(*a, fw);
-        forward.state_out = nullptr;
-        forward.bc = ws;
-        forward.ends = ws + s.ends; forward.dsum = ws + s.end_sums;
-        p.starts = forward.starts = ws + s.starts;
-        rc = launch_scan_forward(*a, forward, fw, false, st);
-        if (rc != DCONV_OK) return rc;
+        p.starts = ws + s.starts;
+        if (pl.chunks > 1) {
+            p.ends = ws + s.ends;
+            p.cum = ws + s.cum;
+        } else {
+            ScanParams forward = p;
+            forward.state_out = nullptr;
+            rc = launch_scan_forward(*a, forward, pl, false, st);
+            if (rc != DCONV_OK) return rc;
+        }
     }
     begin_launch();
     if (a->dtype == DCONV_DTYPE_F16) launch_typed<_Float16>(*a, p, pl.waves, pl.states, st);

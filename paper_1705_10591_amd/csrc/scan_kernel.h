@@ -62,6 +62,8 @@ struct ScanParams {
     const float* bc;
     float *ends, *dsum;              // of the chunks: states [N][chunks][blocks][W][64][R], sums of d [N][chunks][blocks][64]
     float *back;                     // ... and of the way back, laid out like ends
+    float *cum;                      // sums of d from a chunk's start to each tile's [N][tiles][blocks][64], where starts begin
+                                     // every chunk at zero; null where they are the states themselves
     float *part_bc;                  // gradients of B and C: [blocks][N][tiles][2][W][64], see scan_grad.hip
     float *part_A, *part_D, *part_bias;   // [N][chunks][blocks][W][64][R], [N][chunks][blocks][64]
     int N, L, C, S, G, softplus;
