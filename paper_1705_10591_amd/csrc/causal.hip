@@ -28,7 +28,7 @@ struct CausalParams {
 };
 
 // Where a thread works: sequence n, its first channel c and how many of the V exist, its first token.
-struct Place { int n, c, nv, t0, run, strip; int64_t row; bool ok; };
+struct Place { int n, c, nv, t0, run, strip, c0; int64_t row; bool ok, whole; };   // c0: of the workgroup; whole: of the wave
 
 template <int V> __device__ __forceinline__ Place place_of(const CausalParams& p)
 {
@@ -40,11 +40,13 @@ template <int V> __device__ __forceinline__ Place place_of(const CausalParams& p
     a.n = (int)(a.row / p.sgroups);
     a.strip = threadIdx.x / p.vb;
     a.run = threadIdx.x - a.strip * p.vb;
-    a.c = (vg * p.vb + a.run) * V;
+    a.c0 = vg * p.vb * V;
+    a.c = a.c0 + a.run * V;
     a.nv = min(V, p.C - a.c);
     const int64_t t0 = ((int64_t)sg * p.sb + a.strip) * p.strip;
     a.t0 = (int)min(t0, (int64_t)p.L);
     a.ok = a.strip < p.sb && a.nv > 0 && t0 < p.L;
+    a.whole = __all(a.nv == V || !a.ok);             // none of the wave's runs is cut
     return a;
 }
 
@@ -64,12 +66,10 @@ __device__ __forceinline__ void load_filter(const T* filt, int c, int nv, float 
         for (int i = 0; i < V; ++i) w[j][i] = flat[i * F + j];
 }
 
-template <typename T, int F, int V>
-__global__ void __launch_bounds__(kThreads)
-causal_kernel(CausalParams p)
+template <typename T, int F, int V, bool WHOLE>
+__device__ __forceinline__ void causal_strip(const CausalParams& p, Place a)
 {
-    const Place a = place_of<V>(p);
-    if (!a.ok) return;
+    if (WHOLE) a.nv = V;
     const int len = length_of(p.lengths, a.n, p.L), end = min(a.t0 + p.strip, p.L);
     const T* x = (const T*)p.x + a.n * p.x_n + a.c;
     T* out = (T*)p.out + a.n * p.o_n + a.c;
@@ -136,122 +136,141 @@ causal_kernel(CausalParams p)
     }
 }
 
+// (runs that are cut, at the end of a number of channels that V does not divide, have code of their own: branches for them
+// around every load and store are more instructions than the rest)
+template <typename T, int F, int V>
+__global__ void __launch_bounds__(kThreads)
+causal_kernel(CausalParams p)
+{
+    const Place a = place_of<V>(p);
+    if (!a.ok) return;
+    if (a.whole) causal_strip<T, F, V, true>(p, a);
+    else causal_strip<T, F, V, false>(p, a);
+}
+
 // Gradients.  With ds[t] = dout[t] silu'(s[t]) (s computed again): dx[r] = sum_j filt[j] ds[r + F-1-j], so a row of dx is
 // done F-1 tokens later and a strip walks F-1 tokens beyond its end; dfilt[j] = sum_t ds[t] x[t-(F-1)+j] and
 // dbias = sum_t ds[t] are summed over the strip by each thread, over the strips of a workgroup in LDS, and by
 // causal_sum_kernel over workgroups, always in the same order.  Bound by memory like the convolution: x and dout
 // in, dx out.
+template <typename T, int F, int V, bool WHOLE>
+__device__ __forceinline__ void causal_grad_strip(const CausalParams& p, Place a, float (&acc)[F + 1][V])
+{
+    if (WHOLE) a.nv = V;
+    const int len = length_of(p.lengths, a.n, p.L), end = min(a.t0 + p.strip, p.L);
+    const T* x = (const T*)p.x + a.n * p.x_n + a.c;
+    const T* dout = (const T*)p.dout + a.n * p.g_n + a.c;
+    T* dx = (T*)p.dx + a.n * p.d_n + a.c;
+    const int64_t first = (int64_t)a.n * (F - 1) * p.C + a.c;
+    const int stop = (int)min((int64_t)end + F - 1, (int64_t)kMaxTokens + 16);
+    Run<T, V> xn[kGradAhead], gn[kGradAhead], before[F];
+    auto fetch = [&](int t0) {                   // (as in causal_kernel)
+        if (len == 0) return;
+#pragma unroll
+        for (int k = 0; k < kGradAhead; ++k) {
+            xn[k] = load_some<V>(x + min(t0 + k, len - 1) * p.x_l, a.nv);
+            gn[k] = load_some<V>(dout + min(t0 + k, len - 1) * p.g_l, a.nv);
+        }
+    };
+#pragma unroll
+    for (int r = 0; r < F - 1; ++r) {
+        const int t = a.t0 - (F - 1) + r;
+        before[r] = Run<T, V>{};
+        if (t >= 0) {
+            if (len) before[r] = load_some<V>(x + min(t, len - 1) * p.x_l, a.nv);
+        } else if (p.state) {
+            before[r] = load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kGradAhead; ++k) xn[k] = gn[k] = Run<T, V>{};
+    fetch(a.t0);
+    float w[F][V], bias[V] = {}, rows[F][V], ds[F][V] = {};
+    load_filter<T, F, V>((const T*)p.filt, a.c, a.nv, w);
+    if (p.bias) load_some<V>((const T*)p.bias + a.c, a.nv, bias);
+#pragma unroll
+    for (int r = 0; r < F - 1; ++r)              // rows[1 ..]: they move down by one before each token
+#pragma unroll
+        for (int i = 0; i < V; ++i) rows[r + 1][i] = before[r][i];
+    for (int t0 = a.t0; t0 < stop; t0 += kGradAhead) {
+        Run<T, V> xc[kGradAhead], gc[kGradAhead];
+#pragma unroll
+        for (int k = 0; k < kGradAhead; ++k) {
+            xc[k] = xn[k];
+            gc[k] = gn[k];
+        }
+        if (t0 + kGradAhead < stop) fetch(t0 + kGradAhead);
+#pragma unroll
+        for (int k = 0; k < kGradAhead; ++k) {
+            const int t = t0 + k;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+#pragma unroll
+                for (int j = 0; j < F - 1; ++j) { rows[j][i] = rows[j + 1][i]; ds[j][i] = ds[j + 1][i]; }
+                rows[F - 1][i] = xc[k][i];
+                float s = bias[i], d = gc[k][i];
+#pragma unroll
+                for (int j = 0; j < F; ++j) s = __builtin_fmaf(w[j][i], rows[j][i], s);
+                if (p.silu) {
+                    const float sg = sigmoid(s);
+                    d *= sg * (1.f + s * (1.f - sg));
+                }
+                d = t < len ? d : 0.f;
+                ds[F - 1][i] = d;
+                if (t < end) {
+#pragma unroll
+                    for (int j = 0; j < F; ++j) acc[j][i] = __builtin_fmaf(d, rows[j][i], acc[j][i]);
+                    acc[F][i] += d;
+                }
+            }
+            // the row that has all of its terms now; before token 0 it is one of the state
+            const int r = t - (F - 1);
+            if (r < end && (r >= a.t0 || (a.t0 == 0 && p.dstate))) {
+                float v[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    v[i] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < F; ++j) v[i] = __builtin_fmaf(w[j][i], ds[F - 1 - j][i], v[i]);
+                }
+                const int i = r - len + F - 1;               // of state_out, if it went there
+                if (p.dstate_out && i >= 0 && i < F - 1) {
+                    float e[V];
+                    load_some<V>((const T*)p.dstate_out + first + (int64_t)i * p.C, a.nv, e);
+                    for (int k2 = 0; k2 < V; ++k2) v[k2] += e[k2];
+                }
+                if (r >= 0) store_some<V>(dx + r * p.d_l, a.nv, v);
+                else store_some<V>((T*)p.dstate + first + (int64_t)(F - 1 + r) * p.C, a.nv, v);
+            }
+        }
+    }
+}
+
 template <typename T, int F, int V>
 __global__ void __launch_bounds__(kThreads)
 causal_grad_kernel(CausalParams p)
 {
-    __shared__ float red[kThreads * V];
+    __shared__ float red[kThreads * V * (F + 1)];
     const Place a = place_of<V>(p);
     float acc[F + 1][V] = {};
-    if (a.ok) {
-        const int len = length_of(p.lengths, a.n, p.L), end = min(a.t0 + p.strip, p.L);
-        const T* x = (const T*)p.x + a.n * p.x_n + a.c;
-        const T* dout = (const T*)p.dout + a.n * p.g_n + a.c;
-        T* dx = (T*)p.dx + a.n * p.d_n + a.c;
-        const int64_t first = (int64_t)a.n * (F - 1) * p.C + a.c;
-        const int stop = (int)min((int64_t)end + F - 1, (int64_t)kMaxTokens + 16);
-        Run<T, V> xn[kGradAhead], gn[kGradAhead], before[F];
-        auto fetch = [&](int t0) {                   // (as in causal_kernel)
-            if (len == 0) return;
-#pragma unroll
-            for (int k = 0; k < kGradAhead; ++k) {
-                xn[k] = load_some<V>(x + min(t0 + k, len - 1) * p.x_l, a.nv);
-                gn[k] = load_some<V>(dout + min(t0 + k, len - 1) * p.g_l, a.nv);
-            }
-        };
-#pragma unroll
-        for (int r = 0; r < F - 1; ++r) {
-            const int t = a.t0 - (F - 1) + r;
-            before[r] = Run<T, V>{};
-            if (t >= 0) {
-                if (len) before[r] = load_some<V>(x + min(t, len - 1) * p.x_l, a.nv);
-            } else if (p.state) {
-                before[r] = load_some<V>((const T*)p.state + first + (int64_t)(F - 1 + t) * p.C, a.nv);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kGradAhead; ++k) xn[k] = gn[k] = Run<T, V>{};
-        fetch(a.t0);
-        float w[F][V], bias[V] = {}, rows[F][V], ds[F][V] = {};
-        load_filter<T, F, V>((const T*)p.filt, a.c, a.nv, w);
-        if (p.bias) load_some<V>((const T*)p.bias + a.c, a.nv, bias);
-#pragma unroll
-        for (int r = 0; r < F - 1; ++r)              // rows[1 ..]: they move down by one before each token
-#pragma unroll
-            for (int i = 0; i < V; ++i) rows[r + 1][i] = before[r][i];
-        for (int t0 = a.t0; t0 < stop; t0 += kGradAhead) {
-            Run<T, V> xc[kGradAhead], gc[kGradAhead];
-#pragma unroll
-            for (int k = 0; k < kGradAhead; ++k) {
-                xc[k] = xn[k];
-                gc[k] = gn[k];
-            }
-            if (t0 + kGradAhead < stop) fetch(t0 + kGradAhead);
-#pragma unroll
-            for (int k = 0; k < kGradAhead; ++k) {
-                const int t = t0 + k;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-#pragma unroll
-                    for (int j = 0; j < F - 1; ++j) { rows[j][i] = rows[j + 1][i]; ds[j][i] = ds[j + 1][i]; }
-                    rows[F - 1][i] = xc[k][i];
-                    float s = bias[i], d = gc[k][i];
-#pragma unroll
-                    for (int j = 0; j < F; ++j) s = __builtin_fmaf(w[j][i], rows[j][i], s);
-                    if (p.silu) {
-                        const float sg = sigmoid(s);
-                        d *= sg * (1.f + s * (1.f - sg));
-                    }
-                    d = t < len ? d : 0.f;
-                    ds[F - 1][i] = d;
-                    if (t < end) {
-#pragma unroll
-                        for (int j = 0; j < F; ++j) acc[j][i] = __builtin_fmaf(d, rows[j][i], acc[j][i]);
-                        acc[F][i] += d;
-                    }
-                }
-                // the row that has all of its terms now; before token 0 it is one of the state
-                const int r = t - (F - 1);
-                if (r < end && (r >= a.t0 || (a.t0 == 0 && p.dstate))) {
-                    float v[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        v[i] = 0.f;
-#pragma unroll
-                        for (int j = 0; j < F; ++j) v[i] = __builtin_fmaf(w[j][i], ds[F - 1 - j][i], v[i]);
-                    }
-                    const int i = r - len + F - 1;               // of state_out, if it went there
-                    if (p.dstate_out && i >= 0 && i < F - 1) {
-                        float e[V];
-                        load_some<V>((const T*)p.dstate_out + first + (int64_t)i * p.C, a.nv, e);
-                        for (int k2 = 0; k2 < V; ++k2) v[k2] += e[k2];
-                    }
-                    if (r >= 0) store_some<V>(dx + r * p.d_l, a.nv, v);
-                    else store_some<V>((T*)p.dstate + first + (int64_t)(F - 1 + r) * p.C, a.nv, v);
-                }
-            }
-        }
-    }
+    if (a.ok && a.whole) causal_grad_strip<T, F, V, true>(p, a, acc);
+    else if (a.ok) causal_grad_strip<T, F, V, false>(p, a, acc);
     if (!p.part) return;
+    // [strip][filter tap, or bias][channel]
+    const int wide = p.vb * V, values = wide * (F + 1);
+    if (a.strip < p.sb) {
 #pragma unroll
-    for (int q = 0; q <= F; ++q) {
-        __syncthreads();
+        for (int q = 0; q <= F; ++q)
 #pragma unroll
-        for (int i = 0; i < V; ++i) red[threadIdx.x * V + i] = acc[q][i];
-        __syncthreads();
-        if (a.strip == 0 && a.nv > 0) {
-            float* to = p.part + (a.row * (F + 1) + q) * p.C + a.c;
-            for (int i = 0; i < V; ++i) {
-                float s = 0.f;
-                for (int k = 0; k < p.sb; ++k) s += red[(k * p.vb + a.run) * V + i];
-                if (i < a.nv) to[i] = s;
-            }
-        }
+            for (int i = 0; i < V; ++i) red[(a.strip * (F + 1) + q) * wide + a.run * V + i] = acc[q][i];
+    }
+    __syncthreads();
+    float* part = p.part + a.row * (F + 1) * p.C + a.c0;
+    for (int at = threadIdx.x; at < values; at += kThreads) {
+        const int q = at / wide, c = at - q * wide;
+        float s = 0.f;
+        for (int k = 0; k < p.sb; ++k) s += red[k * values + at];
+        if (a.c0 + c < p.C) part[(int64_t)q * p.C + c] = s;
     }
 }
 
@@ -263,8 +282,10 @@ causal_sum_kernel(const float* part, int64_t rows, int C, int F, float* dfilt, f
     const int64_t col = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave, cols = (int64_t)(F + 1) * C;
     const int w = threadIdx.x / kWave;
     float s = 0.f;
-    if (col < cols)
+    if (col < cols) {
+#pragma unroll 8
         for (int64_t r = w; r < rows; r += 4) s += part[r * cols + col];
+    }
     red[threadIdx.x] = s;
     __syncthreads();
     if (w || col >= cols) return;
@@ -320,13 +341,8 @@ bool sizes_ok(const dconv_causal_args& a)
            (double)a.N * a.L * a.C < kMaxElements;
 }
 
-// Elements of a run: 16 bytes, half of that in gradients of more than four taps, whose windows and sums of 8 channels
-// would not fit the registers.
-int run_of(const dconv_causal_args& a, bool grad)
-{
-    const int v = 16 / token_bytes(a.dtype);
-    return grad && a.F > 4 && v == 8 ? 4 : v;
-}
+// Elements of a run: 16 bytes; four in gradients, whose windows and sums of eight would leave two waves a SIMD.
+int run_of(const dconv_causal_args& a, bool grad) { return grad ? 4 : 16 / token_bytes(a.dtype); }
 
 // Runs and strips of a workgroup (at most 256 threads, `most` runs) and the length of a strip: long ones read fewer
 // rows twice, short ones fill the chip.
@@ -376,7 +392,7 @@ enum class Form { kPrompt, kGrad, kStep };
 
 template <typename T, int F> int launch(Form form, const CausalParams& p, hipStream_t st)
 {
-    constexpr int V = 16 / sizeof(T), VG = V == 8 && F > 4 ? 4 : V;
+    constexpr int V = 16 / sizeof(T), VG = 4;
     if (p.total > kMaxBlocks) return DCONV_BAD_SHAPE;
     const dim3 grid((unsigned)p.total);
     begin_launch();

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
+from functools import lru_cache
 from typing import NamedTuple, Optional
 
 import torch
@@ -143,8 +144,23 @@ def _cache(t, tail, dtype, index, what, rows, slots):
     return _dense(t, (M, *tail), dtype, index, what), M
 
 
-def _workspace(bytes_, index):
-    return torch.empty(max(bytes_, 16), dtype=torch.uint8, device=f"cuda:{index}")
+@lru_cache(maxsize=4096)
+def _causal_bytes(code, N, L, C, F):
+    return _lib().dconv_causal_workspace(_CAUSAL.pack(code, N, L, C, F, 0, 0, 0, *(4 * _NONE), *(12 * (0,))))
+
+
+@lru_cache(maxsize=4096)
+def _scan_bytes(code, N, L, C, S, G, form):
+    """Of the workspace of a prompt ("scan"), a gradient with and without starts ("grad", "starts grad"), of the starts."""
+    args = _SCAN.pack(code, N, L, C, S, G, 0, 0, *(12 * _NONE), *(10 * (0,)), 16 if form == "starts grad" else 0, 0, 0, 0, 0)
+    if form == "starts":
+        return _lib().dconv_scan_starts(args)
+    return _lib().dconv_scan_workspace(args, 0 if form == "scan" else 1)
+
+
+def _workspace(bytes_, like):
+    """From torch's allocator, in units of an fp32 element; a size that is not valid is refused by the call itself."""
+    return like.new_empty((max(bytes_, 16) + 3) // 4, dtype=_FLOAT32)
 
 
 class CausalGrad(NamedTuple):
@@ -191,7 +207,7 @@ def dconv_causal(x: torch.Tensor, filt: torch.Tensor, bias: torch.Tensor | None 
         *_rows(x, (N, L, C), dtype, index, "x"), *_rows(out, (N, L, C), dtype, index, "out"), *_NONE, *_NONE,
         _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
         _dense(state, rows, dtype, index, "state"), _dense(state_out, rows, dtype, index, "state_out"), 0, 0, 0, 0,
-        _dense(lengths, (N,), torch.int32, index, "lengths"), 0, 0, 0)
+        _dense(lengths, (N,), _INT32, index, "lengths"), 0, 0, 0)
     _run(_lib().dconv_causal, index, args)
     return out
 
@@ -211,20 +227,18 @@ def dconv_causal_grad(dout: torch.Tensor, x: torch.Tensor, filt: torch.Tensor, b
     else:
         _fits(dx, x.shape, dtype, index, "dx")
         _apart(dx, "dx")
-    sums = torch.empty(C * (F + 1), dtype=torch.float32, device=x.device)
-    dfilt, dbias = sums[:C * F].view(C, F), sums[C * F:]
-    dstate = None if state is None else torch.empty(rows, dtype=dtype, device=x.device)
-    fn = _lib()
-    head = (code, N, L, C, F, 0, bool(silu), 0,
-            *_rows(x, (N, L, C), dtype, index, "x"), *_NONE, *_rows(dout, (N, L, C), dtype, index, "dout"),
-            *_rows(dx, (N, L, C), dtype, index, "dx"),
-            _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
-            _dense(state, rows, dtype, index, "state"), 0, _dense(dstate_out, rows, dtype, index, "dstate_out"),
-            0 if dstate is None else dstate.data_ptr(), dfilt.data_ptr(), dbias.data_ptr(),
-            _dense(lengths, (N,), torch.int32, index, "lengths"), 0)
-    need = fn.dconv_causal_workspace(_CAUSAL.pack(*head, 0, 0))
-    ws = _workspace(need, index)
-    _run(fn.dconv_causal_grad, index, _CAUSAL.pack(*head, ws.data_ptr(), need))
+    dfilt, dbias = x.new_empty((C, F), dtype=_FLOAT32), x.new_empty((C,), dtype=_FLOAT32)
+    dstate = None if state is None else x.new_empty(rows)
+    need = _causal_bytes(code, N, L, C, F)
+    ws = _workspace(need, x)
+    _run(_lib().dconv_causal_grad, index, _CAUSAL.pack(
+        code, N, L, C, F, 0, bool(silu), 0,
+        *_rows(x, (N, L, C), dtype, index, "x"), *_NONE, *_rows(dout, (N, L, C), dtype, index, "dout"),
+        *_rows(dx, (N, L, C), dtype, index, "dx"),
+        _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
+        _dense(state, rows, dtype, index, "state"), 0, _dense(dstate_out, rows, dtype, index, "dstate_out"),
+        0 if dstate is None else dstate.data_ptr(), dfilt.data_ptr(), dbias.data_ptr(),
+        _dense(lengths, (N,), _INT32, index, "lengths"), 0, ws.data_ptr(), need))
     return CausalGrad(dx, dfilt, dbias, dstate)
 
 
@@ -278,7 +292,7 @@ def _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index):
 
 def scan_starts(N: int, L: int, C: int, S: int, G: int = 1, device="cuda") -> torch.Tensor:
     """An empty tensor for the `starts` of dconv_scan and dconv_scan_grad on sequences of these sizes."""
-    need = _lib().dconv_scan_starts(_SCAN.pack(DTYPE_F32, N, L, C, S, G, 0, 0, *(12 * _NONE), *(15 * (0,))))
+    need = _scan_bytes(DTYPE_F32, N, L, C, S, G, "starts")
     if need < 0:
         _bad_shape()
     return torch.empty(need // 4, dtype=torch.float32, device=device)
@@ -287,7 +301,7 @@ def scan_starts(N: int, L: int, C: int, S: int, G: int = 1, device="cuda") -> to
 def _starts(starts, N, L, C, S, G, index):
     if starts is None:
         return 0
-    need = _lib().dconv_scan_starts(_SCAN.pack(DTYPE_F32, N, L, C, S, G, 0, 0, *(12 * _NONE), *(15 * (0,))))
+    need = _scan_bytes(DTYPE_F32, N, L, C, S, G, "starts")
     return _dense(starts, (max(need, 0) // 4,), torch.float32, index, "starts")
 
 
@@ -312,15 +326,14 @@ def dconv_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.T
     else:
         _fits(out, wide, dtype, index, "out")
         _apart(out, "out")
-    head = (code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
+    need = _scan_bytes(code, N, L, ch, S, G, "scan")
+    ws = _workspace(need, u)
+    _run(_lib().dconv_scan, index, _SCAN.pack(
+            code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
             *_rows(out, wide, dtype, index, "out"), *bc[0], *bc[1], *(6 * _NONE), *params,
             _dense(state, (N, ch, S), torch.float32, index, "state"),
             _dense(state_out, (N, ch, S), torch.float32, index, "state_out"), 0, 0, 0, 0, 0,
-            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), torch.int32, index, "lengths"), 0)
-    fn = _lib()
-    need = fn.dconv_scan_workspace(_SCAN.pack(*head, 0, 0), 0)
-    ws = _workspace(need, index)
-    _run(fn.dconv_scan, index, _SCAN.pack(*head, ws.data_ptr(), need))
+            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"), 0, ws.data_ptr(), need))
     return out
 
 
@@ -338,33 +351,31 @@ def dconv_scan_grad(dout: torch.Tensor, u: torch.Tensor, delta: torch.Tensor, A:
     N, L, ch = u.shape
     wide, narrow = (N, L, ch), (N, L, G, S)
     tokens, bc, params = _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index)
-    make = lambda shape, t=dtype: torch.empty(shape, dtype=t, device=u.device)
     for t, what in ((du, "du"), (ddelta, "ddelta"), (dz, "dz")):
         if t is not None:
             _fits(t, wide, dtype, index, what)
             _apart(t, what)
-    du = make(wide) if du is None else du
-    ddelta = make(wide) if ddelta is None else ddelta
+    du = u.new_empty(wide) if du is None else du
+    ddelta = u.new_empty(wide) if ddelta is None else ddelta
     if z is None:
         dz = None
     elif dz is None:
-        dz = make(wide)
-    dB, dC, dA = make(narrow), make(narrow), make((ch, S), torch.float32)
-    dD = None if D is None else make((ch,), torch.float32)
-    dbias = None if delta_bias is None else make((ch,), torch.float32)
-    dstate = None if state is None else make((N, ch, S), torch.float32)
+        dz = u.new_empty(wide)
+    dB, dC, dA = u.new_empty(narrow), u.new_empty(narrow), A.new_empty((ch, S))
+    dD = None if D is None else A.new_empty((ch,))
+    dbias = None if delta_bias is None else A.new_empty((ch,))
+    dstate = None if state is None else A.new_empty((N, ch, S))
     ptr = lambda t: 0 if t is None else t.data_ptr()
-    head = (code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2], *_NONE, *bc[0], *bc[1],
+    need = _scan_bytes(code, N, L, ch, S, G, "grad" if starts is None else "starts grad")
+    ws = _workspace(need, u)
+    _run(_lib().dconv_scan_grad, index, _SCAN.pack(
+            code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2], *_NONE, *bc[0], *bc[1],
             *_rows(dout, wide, dtype, index, "dout"), *_rows(du, wide, dtype, index, "du"),
             *_rows(ddelta, wide, dtype, index, "ddelta"), *_rows(dz, wide, dtype, index, "dz"),
             *_rows(dB, narrow, dtype, index, "dB"), *_rows(dC, narrow, dtype, index, "dC"), *params,
             _dense(state, (N, ch, S), torch.float32, index, "state"), 0,
             _dense(dstate_out, (N, ch, S), torch.float32, index, "dstate_out"), ptr(dstate), ptr(dA), ptr(dD), ptr(dbias),
-            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), torch.int32, index, "lengths"), 0)
-    fn = _lib()
-    need = fn.dconv_scan_workspace(_SCAN.pack(*head, 0, 0), 1)
-    ws = _workspace(need, index)
-    _run(fn.dconv_scan_grad, index, _SCAN.pack(*head, ws.data_ptr(), need))
+            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"), 0, ws.data_ptr(), need))
     return ScanGrad(du, ddelta, dA, dB, dC, dD, dz, dbias, dstate)
 
 
