@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
+import sys
 from functools import lru_cache
 from typing import NamedTuple, Optional
 
@@ -43,29 +44,28 @@ def declare(lib: ctypes.CDLL) -> None:
             fn.restype = ctypes.c_int
 
 
-_loaded = None
+_loaded = _package = None
 
 
 def _lib():
-    global _loaded
+    global _loaded, _package
     if _loaded is None:
-        from . import load_library
-        _loaded = load_library()
+        _package = sys.modules[__package__]
+        _loaded = _package.load_library()
     return _loaded
 
 
 def _run(fn, index, args):
-    from . import _enqueue, _raise, _raw_stream
     if index != _device():
-        return _enqueue(fn, index, args)
-    rc = fn(args, _raw_stream(index))
+        return _package._enqueue(fn, index, args)
+    rc = fn(args, _package._raw_stream(index))
     if rc:
-        _raise(rc)
+        _package._raise(rc)
 
 
 def _bad_shape():
-    from . import STATUS_BAD_SHAPE, _raise
-    _raise(STATUS_BAD_SHAPE)
+    _lib()
+    _package._raise(_package.STATUS_BAD_SHAPE)
 
 
 def _first(t, dims, what):
@@ -136,12 +136,13 @@ def _dense(t, shape, dtype, index, what):
 
 def _cache(t, tail, dtype, index, what, rows, slots):
     """(pointer, rows) of a cache of states that a step updates."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.shape[1:] != tail:
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{what} must have the shape (rows, {', '.join(map(str, tail))})")
     M = t.shape[0]
+    p = _dense(t, (M, *tail), dtype, index, what)
     if M == 0 or (slots is None and M < rows):
         raise ValueError(f"{what} has too few rows")
-    return _dense(t, (M, *tail), dtype, index, what), M
+    return p, M
 
 
 @lru_cache(maxsize=4096)
