@@ -29,17 +29,13 @@ bc_kernel(Rows B, Rows C, int64_t b_g, int64_t c_g, const int* lengths, float* b
 // OUT: the outputs of all tokens, with the states wanted on the way; otherwise the states alone, and with `ends` those of each chunk
 // begun at zero (the first at the call's state, which is kept for the second launch in the last chunk's place).
 // WHOLE: the block has 64 channels, so that no run of them is cut.
-// AHEAD: while a tile's recurrence runs, the one before it is finished (sums over waves, gate, store) and the one after it
-// prepared (d, d u): two of everything in LDS, one barrier a tile, and work between the recurrence's dependent
-// instructions.  That is for launches of few waves; where there are many, they fill each other's gaps and twice
-// the LDS would keep some of them away.
-template <int W, bool OUT, bool AHEAD> struct ScanLds {
-    float2 step[AHEAD ? 2 : 1][kT][kWave];              // d, d u
-    float ysum[AHEAD && OUT ? 2 : 1][OUT ? W : 1][kT][kWave];
+template <int W, bool OUT> struct ScanLds {
+    float2 step[kT][kWave];                             // d, d u
+    float ysum[OUT ? W : 1][kT][kWave];
 };
 
-template <typename T, int W, int R, bool OUT, bool AHEAD, bool WHOLE>
-__device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace& a, ScanLds<W, OUT, AHEAD>& lds, bool ends)
+template <typename T, int W, int R, bool OUT, bool WHOLE>
+__device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace& a, ScanLds<W, OUT>& lds, bool ends)
 {
     constexpr int E = kT / W;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -83,7 +79,7 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
     Share<const T, E> pu(p.u, a.n, t, ec), pd(p.delta, a.n, t, ec), pz(p.z, a.n, t, ec);
     Share<T, E> po(p.out, a.n, t, ec);
     pu.spare(); pd.spare(); pz.spare(); po.spare();
-    Run<T, E> u{}, dl{}, z{}, uc{}, zc{}, ul{}, zl{};     // of the tile fetched, the one at hand, the last one
+    Run<T, E> u{}, dl{}, z{}, ul{}, zl{};                 // of the tile fetched, the one at hand
     auto fetch = [&](int at) {
         if (at < a.len && nv > 0) {
             u = pu.load(nv);
@@ -107,17 +103,16 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
             }
         }
 #pragma unroll
-        for (int i = 0; i < E; ++i) lds.step[AHEAD ? tile & 1 : 0][tt][tc + i] = make_float2(d_[i], d_[i] * u_[i]);
+        for (int i = 0; i < E; ++i) lds.step[tt][tc + i] = make_float2(d_[i], d_[i] * u_[i]);
     };
-    auto finish = [&](int tile, int at) {                 // the last tile
-        if (!OUT) return;
+    auto finish = [&](int tile, int at) {                 // the tile at hand: sums over waves, gate
         if (nv > 0 && at < p.L) {
             float y[E];
 #pragma unroll
             for (int i = 0; i < E; ++i) y[i] = skip[i] * ul[i];
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                const Run<float, E> part = lds_run<E>(&lds.ysum[AHEAD && OUT ? tile & 1 : 0][w][tt][tc]);
+                const Run<float, E> part = lds_run<E>(&lds.ysum[w][tt][tc]);
 #pragma unroll
                 for (int i = 0; i < E; ++i) y[i] += part[i];
             }
@@ -139,37 +134,31 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
     if (a.tile0 < a.stop) {
         fetch(t);
         bc.load(bc_of(p, a, a.tile0, W, wave));
-        if (AHEAD) {
-            prepare(a.tile0, t);
-            uc = u; zc = z;
-            if (a.tile0 + 1 < a.stop) fetch(t + kT);
-            meet();
-        }
     }
     for (int tile = a.tile0; tile < a.stop; ++tile, t += kT) {
-        const auto& step = lds.step[AHEAD ? tile & 1 : 0];
-        auto& ysum = lds.ysum[AHEAD && OUT ? tile & 1 : 0];
-        if (!AHEAD) {
-            prepare(tile, t);
-            ul = u; zl = z;
-            if (tile + 1 < a.stop) fetch(t + kT);
-            meet();
-        }
+        const auto& step = lds.step;
+        auto& ysum = lds.ysum;
+        prepare(tile, t);
+        ul = u; zl = z;
+        if (tile + 1 < a.stop) fetch(t + kT);
+        meet();
         if (p.starts && !ends) store_states(p.starts + lane_states<W, R>(p, a, (int64_t)a.n * p.tiles + tile, wave, lane), h);
         float2 d[kStep], dn[kStep];
+        float ys[kStep];
 #pragma unroll
         for (int k = 0; k < kStep; ++k) d[k] = step[k][lane];
         const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, min(tile + 1, a.stop - 1), W, wave);
 #pragma unroll
         for (int k0 = 0; k0 < kT; k0 += kStep) {
             const bool more = k0 + kStep < kT;
+            arrived();
             next.load(more ? here + k0 + kStep : after);
 #pragma unroll
-            for (int k = 0; k < kStep; ++k)
+            for (int k = 0; k < kStep; ++k) {
                 if (more) dn[k] = step[k0 + kStep + k][lane];
+                if (OUT && k0) ysum[wave][k0 - kStep + k][lane] = ys[k];
+            }
             in_order();
-            if (AHEAD && k0 == 0 && tile > a.tile0) finish(tile - 1, t - kT);
-            if (AHEAD && k0 == 2 * kStep && tile + 1 < a.stop) prepare(tile + 1, t + kT);
 #pragma unroll
             for (int k = 0; k < kStep; ++k) {
                 float y = 0.f;
@@ -178,7 +167,7 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
                     h[r] = __builtin_fmaf(exp2_(d[k].x * A[r]), h[r], d[k].y * bc.b(k, r));
                     if (OUT) y = r ? __builtin_fmaf(bc.c(k, r), h[r], y) : bc.c(k, r) * h[r];
                 }
-                if (OUT) ysum[wave][k0 + k][lane] = y;
+                if (OUT) ys[k] = y;
                 else dtotal += d[k].x;
             }
             in_order();
@@ -186,17 +175,13 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
 #pragma unroll
             for (int k = 0; k < kStep; ++k) d[k] = dn[k];
         }
-        if (AHEAD) {
-            ul = uc; zl = zc;
-            uc = u; zc = z;
-            if (tile + 2 < a.stop) fetch(t + 2 * kT);
-            meet();
-        } else {
-            meet();
-            finish(tile, t);
+        if (OUT) {
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) ysum[wave][kT - kStep + k][lane] = ys[k];
         }
+        meet();
+        if (OUT) finish(tile, t);
     }
-    if (AHEAD && a.tile0 < a.stop) finish(a.stop - 1, t - kT);
     if (OUT && nv > 0) {
         const float zero[E] = {};
         for (int tile = a.stop; tile < a.tile1; ++tile, t += kT, po.forward())       // tiles that do not count
@@ -210,27 +195,22 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
     }
 }
 
-template <typename T, int W, int R, bool OUT, bool AHEAD>
+template <typename T, int W, int R, bool OUT>
 __global__ void __launch_bounds__(kWave * W)
 scan_kernel(ScanParams p, bool ends)
 {
-    __shared__ ScanLds<W, OUT, AHEAD> lds;
+    __shared__ ScanLds<W, OUT> lds;
     const ScanPlace a = scan_place(p);
-    if (a.nc == kWave) scan_block<T, W, R, OUT, AHEAD, true>(p, a, lds, ends);
-    else scan_block<T, W, R, OUT, AHEAD, false>(p, a, lds, ends);
+    if (a.nc == kWave) scan_block<T, W, R, OUT, true>(p, a, lds, ends);
+    else scan_block<T, W, R, OUT, false>(p, a, lds, ends);
 }
 
 template <typename T, int W, int R>
 void launch_kernel(const ScanParams& p, bool out, bool ends, int64_t blocks, hipStream_t st)
 {
     const dim3 grid((unsigned)blocks), threads(kWave * W);
-    // Measured, 16 states, us ahead and not: 64 workgroups of 64 tiles 110, 134; 512 of 128 324, 344; 768 426, 451; 1024 583, 555;
-    // 4 states: 512 of 64 118, 123; 1024 255, 177.
-    const bool ahead = blocks * W < (R == 4 ? 3584 : 3072);
-    if (out && ahead) hipLaunchKernelGGL((scan_kernel<T, W, R, true, true>), grid, threads, 0, st, p, false);
-    else if (out) hipLaunchKernelGGL((scan_kernel<T, W, R, true, false>), grid, threads, 0, st, p, false);
-    else if (ahead) hipLaunchKernelGGL((scan_kernel<T, W, R, false, true>), grid, threads, 0, st, p, ends);
-    else hipLaunchKernelGGL((scan_kernel<T, W, R, false, false>), grid, threads, 0, st, p, ends);
+    if (out) hipLaunchKernelGGL((scan_kernel<T, W, R, true>), grid, threads, 0, st, p, false);
+    else hipLaunchKernelGGL((scan_kernel<T, W, R, false>), grid, threads, 0, st, p, ends);
 }
 
 template <typename T>
@@ -265,8 +245,10 @@ bool scan_sizes_ok(const dconv_scan_args& a)
     // (sizes in floating point, so that no product overflows)
     if ((double)a.N * a.L * a.C * kMaxStates >= kMaxElements) return false;
     const ScanPlan pl = scan_plan(a, false);             // (a gradient has no more chunks)
-    return (double)a.N * pl.blocks * pl.chunks <= 2147483647.0 &&
-           (double)a.N * a.G * pl.tiles * kT * pl.waves <= 2147483647.0 * kThreads;
+    // (workgroups of the largest grids: the scans', bc_kernel's, the sums')
+    const double bc = (double)a.N * a.G * pl.tiles * pl.waves;
+    return (double)a.N * pl.blocks * pl.chunks <= 2147483647.0 && bc * kT / kThreads <= 2147483646.0 &&
+           bc * (kT / 8 * kWave) / kThreads + pl.blocks * (kMaxStates + 2.0) <= 2147483646.0;
 }
 
 ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
@@ -279,15 +261,16 @@ ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
     pl.blocks = a.G * pl.gblocks;
     pl.tiles = (a.L + kT - 1) / kT;
     // Chunks cost another launch that does most of the work again, so there are none where the channels alone give the
-    // chip one and a half waves a SIMD (gradients: nearly two), nor for a few tiles.  Otherwise as many as give it eight
-    // (gradients, whose registers let two be there at a time: four) in chunks of four tiles or more, or half of that in chunks
-    // of two.  Measured with 16 states, us for 1 chunk and for the rule's (sequences x tokens x channels):
-    //   scan      1 x 256 x 2048   32, 25   1 x 4096 x 4096   431, 135   3 x 2048 x 4096  221, 181   8 x 2048 x 4096   325, (404)
-    //   gradient  1 x 256 x 2048  104, 56   1 x 4096 x 4096  1267, 418   4 x 2048 x 4096  818, 740   8 x 2048 x 4096  1179, (1310)
+    // chip one and a half waves a SIMD (gradients, whose registers let two be there at a time: two), nor for a few tiles.
+    // Otherwise as many as give it eight (gradients: four, and four chunks at least) in chunks of four tiles or more, or
+    // half of that in chunks of two.  Measured with 16 states, us for 1 chunk and for the rule's (sequences x tokens x channels):
+    //   scan      1 x 256 x 2048   32, 25   1 x 4096 x 4096   447, 137   3 x 2048 x 4096  227, 177   8 x 2048 x 4096   324, (400)
+    //   gradient  1 x 256 x 2048  104, 50   1 x 4096 x 4096  1500, 350   4 x 2048 x 4096  819, 648   8 x 2048 x 4096  1193, (1205)
     const double alone = (double)a.N * pl.blocks * pl.waves;
     pl.chunks = 1;
-    if (alone < (grad ? 1792 : 1536) && pl.tiles >= (grad ? 6 : 10)) {
-        const int most = grad ? (int)(4096 / alone) : (int)(8192 / alone);
+    if (alone < (grad ? 2048 : 1536) && pl.tiles >= (grad ? 6 : 10)) {
+        int most = (int)((grad ? 4096 : 8192) / alone);
+        if (grad && most < 4) most = 4;
         const int longer = most < pl.tiles / 4 ? most : pl.tiles / 4, shorter = most / 2 < pl.tiles / 2 ? most / 2 : pl.tiles / 2;
         pl.chunks = longer > shorter ? longer : shorter;
         if (pl.chunks < 2) pl.chunks = 1;

@@ -113,6 +113,7 @@ __device__ __forceinline__ void back_block(const ScanParams& p, const ScanPlace&
         const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, max(tile - 1, a.tile0), W, wave);
 #pragma unroll
         for (int k0 = kT - kStep; k0 >= 0; k0 -= kStep) {
+            arrived();
             next.load(k0 ? here + k0 - kStep : after + kT - kStep);
 #pragma unroll
             for (int k = 0; k < kStep; ++k)
@@ -234,6 +235,7 @@ __device__ __forceinline__ void sweep_block(const ScanParams& p, const ScanPlace
 #pragma unroll
         for (int k0 = 0; k0 < kT; k0 += kStep) {
             const bool more = k0 + kStep < kT;
+            arrived();
             next.load(more ? here + k0 + kStep : after);
 #pragma unroll
             for (int k = 0; k < kStep; ++k) {
@@ -402,15 +404,19 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
         const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, max(tile - 1, a.tile0), W, wave);
         float dec[kT][R], h[kT][R];
         float2 s[kStep], sn[kStep];
+        float ys[kStep], qs[kStep];
 #pragma unroll
         for (int k = 0; k < kStep; ++k) s[k] = step[k][lane];
 #pragma unroll
         for (int k0 = 0; k0 < kT; k0 += kStep) {
             const bool more = k0 + kStep < kT;
+            arrived();
             if (more) next.load(here + k0 + kStep);
 #pragma unroll
-            for (int k = 0; k < kStep; ++k)
+            for (int k = 0; k < kStep; ++k) {
                 if (more) sn[k] = step[k0 + kStep + k][lane];
+                if (k0) sums[0][wave][k0 - kStep + k][lane] = ys[k];
+            }
             in_order();
 #pragma unroll
             for (int k = k0; k < k0 + kStep; ++k) {
@@ -421,7 +427,7 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
                     h[k][r] = __builtin_fmaf(dec[k][r], k ? h[k - 1][r] : h0[r], s[k - k0].y * bc.b(k - k0, r));
                     y = r ? __builtin_fmaf(bc.c(k - k0, r), h[k][r], y) : bc.c(k - k0, r) * h[k][r];
                 }
-                sums[0][wave][k][lane] = y;
+                ys[k - k0] = y;
             }
             in_order();
             if (more) {
@@ -432,12 +438,20 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
         }
         float packed[kGather], dy[kStep], dyn[kStep];
 #pragma unroll
-        for (int k = 0; k < kStep; ++k) dy[k] = gout[kT - kStep + k][lane];
+        for (int k = 0; k < kStep; ++k) {
+            dy[k] = gout[kT - kStep + k][lane];
+            sums[0][wave][kT - kStep + k][lane] = ys[k];
+        }
 #pragma unroll
         for (int k0 = kT - kStep; k0 >= 0; k0 -= kStep) {
+            arrived();
             next.load(k0 ? here + k0 - kStep : after);
 #pragma unroll
             for (int k = 0; k < kStep; ++k) {
+                if (k0 < kT - kStep) {
+                    sums[1][wave][k0 + kStep + k][lane] = qs[k];
+                    sums[2][wave][k0 + kStep + k][lane] = ys[k];
+                }
                 if (!k0) continue;
                 sn[k] = step[k0 - kStep + k][lane];
                 dyn[k] = gout[k0 - kStep + k][lane];
@@ -457,8 +471,8 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
                     dA[r] = __builtin_fmaf(e, s[j].x, dA[r]);
                     pair[r] = fold32(g * s[j].y, dy[j] * h[k][r]);
                 }
-                sums[1][wave][k][lane] = q;
-                sums[2][wave][k][lane] = ea;
+                qs[j] = q;
+                ys[j] = ea;
                 // lane bit 5: B or C; bits 4 and 3 the state, the rest the token, as far as there are states
                 if constexpr (R == 4) packed[k & 7] = fold<kAcross8>(fold16(pair[0], pair[2]), fold16(pair[1], pair[3]), lane & 8);
                 else packed[k] = fold16(pair[0], pair[R - 1]);
@@ -484,6 +498,11 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
                 s[k] = sn[k];
                 dy[k] = dyn[k];
             }
+        }
+#pragma unroll
+        for (int k = 0; k < kStep; ++k) {
+            sums[1][wave][k][lane] = qs[k];
+            sums[2][wave][k][lane] = ys[k];
         }
         meet();
         if (nv > 0 && t < p.L) {
@@ -567,35 +586,10 @@ scan_grad_kernel(ScanParams p)
     else grad_block<T, W, R, false>(p, a, lds);
 }
 
-// dB and dC from the parts of a group's channel blocks; lane l of a unit has the value that lane l had above.
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-scan_sum_bc_kernel(const float* part, Rows dB, Rows dC, int64_t b_g, int64_t c_g, const int* lengths, int N, int L, int G, int S,
-                   int W, int R, int tiles, int gblocks)
+// What many workgroups have a part of, in the same order on every call.  The first p.blocks * (W R + 2) workgroups:
+// dA, dD and the gradient of the bias from the parts of all sequences and chunks, four waves a quarter each.
+__device__ __forceinline__ void sum_params(const ScanParams& p, int W, int R, float* dA, float* dD, float* dbias, float (&red)[4][kWave])
 {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int lane = (int)(i & 63);
-    const int tokens = gathered(R);
-    const int64_t unit = i >> 6, per = (int64_t)tiles * (kT / tokens) * W;      // units [G][N][tiles][kT / tokens][W]
-    const int64_t seq = unit / per, in = unit - seq * per;
-    const int g = (int)(seq / N), n = (int)(seq - (int64_t)g * N);
-    if (g >= G) return;
-    const int w = (int)(in % W), t = (int)(in / W) * tokens + (lane & (tokens - 1));
-    const int r = R == 4 ? (lane >> 4 & 1) * 2 + (lane >> 3 & 1) : lane >> 4 & 1, s = w * R + r;
-    if (r >= R) return;
-    if (t >= L || s >= S) return;
-    float v = 0.f;
-    if (t < length_of(lengths, n, L))
-        for (int k = 0; k < gblocks; ++k) v += part[(((int64_t)(g * gblocks + k) * N + n) * per + in) * kWave + lane];
-    if (lane < 32) dB.at<T>(n, t, 0)[g * b_g + s] = (T)v;
-    else dC.at<T>(n, t, 0)[g * c_g + s] = (T)v;
-}
-
-// dA, dD and the gradient of the bias from the parts of all sequences and chunks: four waves take a quarter of them each.
-__global__ void __launch_bounds__(kThreads)
-scan_sum_kernel(ScanParams p, int W, int R, float* dA, float* dD, float* dbias)
-{
-    __shared__ float red[4][kWave];
     const int values = W * R + 2, block = blockIdx.x / values, v = blockIdx.x - block * values;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t rows = (int64_t)p.N * p.chunks;
@@ -619,6 +613,34 @@ scan_sum_kernel(ScanParams p, int W, int R, float* dA, float* dD, float* dbias)
     }
 }
 
+// The others: dB and dC from the parts of a group's channel blocks; lane l of a unit has the value that lane l had above.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+scan_sum_kernel(ScanParams p, int W, int R, float* dA, float* dD, float* dbias, Rows dB, Rows dC, int64_t b_g, int64_t c_g)
+{
+    __shared__ float red[4][kWave];
+    const int first = p.blocks * (W * R + 2);
+    if ((int)blockIdx.x < first) return sum_params(p, W, R, dA, dD, dbias, red);
+    const int64_t i = (int64_t)((int)blockIdx.x - first) * kThreads + threadIdx.x;
+    const int lane = (int)(i & 63), tokens = gathered(R);
+    const int64_t unit = i >> 6, per = (int64_t)p.tiles * (kT / tokens) * W;    // units [G][N][tiles][kT / tokens][W]
+    const int64_t seq = unit / per, in = unit - seq * per;
+    const int g = (int)(seq / p.N), n = (int)(seq - (int64_t)g * p.N);
+    if (g >= p.G) return;
+    const int w = (int)(in % W), t = (int)(in / W) * tokens + (lane & (tokens - 1));
+    const int r = R == 4 ? (lane >> 4 & 1) * 2 + (lane >> 3 & 1) : lane >> 4 & 1, s = w * R + r;
+    if (r >= R || t >= p.L || s >= p.S) return;
+    float v = 0.f;
+    if (t < length_of(p.lengths, n, p.L)) {
+        const float* from = p.part_bc + (((int64_t)g * p.gblocks * p.N + n) * per + in) * kWave + lane;
+        const int64_t step = p.N * per * kWave;
+#pragma unroll 8
+        for (int k = 0; k < p.gblocks; ++k) v += from[k * step];
+    }
+    if (lane < 32) dB.at<T>(n, t, 0)[g * b_g + s] = (T)v;
+    else dC.at<T>(n, t, 0)[g * c_g + s] = (T)v;
+}
+
 template <typename T, int W, int R> void launch_kernels(const ScanParams& p, hipStream_t st)
 {
     if (p.cum)
@@ -635,9 +657,9 @@ template <typename T> void launch_typed(const dconv_scan_args& a, const ScanPara
     else if (a.S <= 16) launch_kernels<T, 4, 4>(p, st);
     else launch_kernels<T, 8, 4>(p, st);
     const int64_t n = (int64_t)p.N * p.G * p.tiles * (kT / gathered(R)) * W * kWave;
-    hipLaunchKernelGGL((scan_sum_bc_kernel<T>), dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p.part_bc,
-                       Rows{a.dB.p, a.dB.sn, a.dB.sl}, Rows{a.dC.p, a.dC.sn, a.dC.sl}, a.dB.sg, a.dC.sg, a.lengths, a.N, a.L,
-                       a.G, a.S, W, R, p.tiles, p.gblocks);
+    hipLaunchKernelGGL((scan_sum_kernel<T>), dim3((unsigned)(p.blocks * (W * R + 2) + (n + kThreads - 1) / kThreads)), dim3(kThreads),
+                       0, st, p, W, R, a.dA, a.dD, a.ddelta_bias, Rows{a.dB.p, a.dB.sn, a.dB.sl}, Rows{a.dC.p, a.dC.sn, a.dC.sl},
+                       a.dB.sg, a.dC.sg);
 }
 
 // The workspace of a gradient call, in floats: where its parts begin, and how many there are.
@@ -708,8 +730,6 @@ int dconv_scan_grad(const dconv_scan_args* a, void* stream)
     if (a->dtype == DCONV_DTYPE_F16) launch_typed<_Float16>(*a, p, pl.waves, pl.states, st);
     else if (a->dtype == DCONV_DTYPE_BF16) launch_typed<__bf16>(*a, p, pl.waves, pl.states, st);
     else launch_typed<float>(*a, p, pl.waves, pl.states, st);
-    hipLaunchKernelGGL(scan_sum_kernel, dim3((unsigned)(pl.blocks * (pl.waves * pl.states + 2))), dim3(kThreads), 0, st, p, pl.waves, pl.states, a->dA, a->dD,
-                       a->ddelta_bias);
     return launch_status();
 }
 

@@ -12,8 +12,8 @@
 //    used, zeros behind the end of a sequence and beyond state S.  With d = 0 there too, tokens that do not count leave the state as it is,
 //    and the loops need no masks.
 //  * Scalar loads come back in any order, so that a wait for one is a wait for all: a tile is walked in steps of kStep = 4
-//    tokens, and the operands of the next step (64 of B and C in scalar registers, d and d u from LDS) are asked for before the
-//    arithmetic of this one.
+//    tokens.  A step waits for its operands, asks for those of the next one (64 of B and C in scalar registers, d and d u from
+//    LDS), writes the sums of the last one, and calculates.
 //  * A call with too few (sequence, channel block) pairs for the chip cuts its sequences into chunks: a first launch
 //    runs each chunk from a state of zero, and each workgroup of the second begins by putting together what the chunks
 //    before it leave, since a chunk changes the state it is given by the factor exp(A sum d) alone.
@@ -120,6 +120,15 @@ template <int E> __device__ __forceinline__ Run<float, E> lds_run(const float* p
 
 // Nothing moves past this point: what is written above it is under way before what is written below begins.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// All scalar loads and LDS operations so far are done (s_waitcnt lgkmcnt(0)).  Without it the wait would come at the first use of
+// a step's operands, behind the requests for the next step's, and wait for those too.
+__device__ __forceinline__ void arrived()
+{
+    in_order();
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    in_order();
+}
 
 // A thread's share of the tiles of a token tensor: one token a tile, E channels.  It walks by whole tiles, so that a tile
 // costs one 64-bit addition.
