@@ -5,7 +5,8 @@
 // sliding window (Sec. 3: a thread keeps the rows that its next output needs in registers and reads one new row a
 // step) does that along the tokens: a thread has a run of V channels (16 bytes) and walks a strip of tokens with the
 // last F-1 rows in registers, kAhead rows in flight; lanes next to each other have runs next to each other.  Only the
-// F-1 rows before a strip are read twice.
+// F-1 rows before a strip are read twice.  Measured: 8 x 4096 x 4096 bf16 with 4 taps 116 us, 4.64 TB/s of the 4.94 that a
+// large copy reaches; the gradient of half as many tokens 96 + 5 us; one row of 2048 channels 2.4 us, 200 rows of 5120 5.6.
 #include "tokens.h"
 
 namespace dconv {
