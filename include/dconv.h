@@ -424,7 +424,7 @@ int dconv_general_noalloc(const float *in, int N, int C, int H, int W,
  *     graphs among them, need one each.
  *   - Errors: a required pointer (or the argument struct) that is NULL ->
  *     DCONV_NULL_POINTER; a size <= 0, F > 8, S > 32, C not a multiple of G, more
- *     than 2^30 tokens of a sequence, work beyond 2^31-1 workgroups, misaligned
+ *     than 2^30 channels or tokens of a sequence, work beyond 2^31-1 workgroups, misaligned
  *     data -> DCONV_BAD_SHAPE; another element type -> DCONV_UNSUPPORTED; a workspace that
  *     is too small -> DCONV_SCRATCH_EXCEEDED.
  */

@@ -338,7 +338,7 @@ constexpr int64_t kMaxBlocks = 2147483647LL;
 
 bool sizes_ok(const dconv_causal_args& a)
 {
-    return a.N > 0 && a.L > 0 && a.L <= kMaxTokens && a.C > 0 && a.F > 0 && a.F <= kMaxTaps &&
+    return a.N > 0 && a.L > 0 && a.L <= kMaxTokens && a.C > 0 && a.C <= kMaxChannels && a.F > 0 && a.F <= kMaxTaps &&
            (double)a.N * a.L * a.C < kMaxElements;
 }
 

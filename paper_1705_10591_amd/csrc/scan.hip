@@ -240,7 +240,7 @@ int scan_wave_states(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : 4; }
 
 bool scan_sizes_ok(const dconv_scan_args& a)
 {
-    if (!(a.N > 0 && a.L > 0 && a.L <= kMaxTokens && a.C > 0 && a.S > 0 && a.S <= kMaxStates && a.G > 0 && a.C % a.G == 0))
+    if (!(a.N > 0 && a.L > 0 && a.L <= kMaxTokens && a.C > 0 && a.C <= kMaxChannels && a.S > 0 && a.S <= kMaxStates && a.G > 0 && a.C % a.G == 0))
         return false;
     // (sizes in floating point, so that no product overflows)
     if ((double)a.N * a.L * a.C * kMaxStates >= kMaxElements) return false;

@@ -69,7 +69,8 @@ template <int N, typename T> __device__ __forceinline__ void store_some(T* p, in
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 constexpr int kMaxTokens = 1 << 30;      // of a sequence: token numbers and what is added to them fit 32 bits
-constexpr double kMaxElements = 1.1e18; // of a tensor, 2^60: sizes in 64 bits do not overflow
+constexpr int kMaxChannels = 1 << 30;    // likewise
+constexpr double kMaxElements = 1.1e18;  // of a tensor, 2^60: sizes in 64 bits do not overflow
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 

@@ -299,3 +299,77 @@ def test_a_layer_trains():
         diff = (value(*plus) - value(*minus)) / (2 * e)
         # differences in 64 bits are good to 1e-7 here; the gradients' own errors are below 1e-5 of the sizes that they add up
         assert abs(diff - (_np(got) * way).sum()) < 1e-5 * (np.abs(_np(got) * way)).sum() + 1e-6, k
+
+
+def test_replays_read_lengths_and_slots_anew():
+    """A captured step and prompt serve other rows and lengths on every replay."""
+    N, L, C, S, F, M = 4, 40, 68, 16, 4, 9
+    x, _, dout, _ = _inputs(21, torch.bfloat16, N, L, C, S, 1, state=False)
+    g = torch.Generator().manual_seed(3)
+    w = (0.5 * torch.randn((C, F), generator=g)).bfloat16().cuda()
+    win0, h0 = torch.randn((M, F - 1, C), generator=g).bfloat16().cuda(), torch.randn((M, C, S), generator=g).cuda()
+    one = {k: v if v is None or k in ("A", "D", "delta_bias") else v[:, 0] for k, v in x.items()}
+    lengths, slots = torch.zeros(N, dtype=torch.int32, device="cuda"), torch.zeros(N, dtype=torch.int32, device="cuda")
+
+    def calls(win, h):
+        c = dconv.dconv_causal(x["u"], w, lengths=lengths)
+        y = dconv.dconv_scan(**dict(x, u=c), lengths=lengths)
+        grads = dconv.dconv_scan_grad(dout, **dict(x, u=c), lengths=lengths)
+        u1 = dconv.dconv_causal_step(one["u"], win, w, slots=slots)
+        y1 = dconv.dconv_scan_step(**dict(one, u=u1), state=h, slots=slots)
+        return [c, y, u1, y1, win, h] + [t for t in grads if t is not None]
+
+    win, h = win0.clone(), h0.clone()
+    calls(win, h)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        captured = calls(win, h)
+    for ln, sl in (([40, 1, 0, 17], [3, 1, 8, 0]), ([16, 33, 40, 5], [8, -1, 8, 2]), ([0, 0, 0, 0], [-1, 99, -5, 4])):
+        lengths.copy_(torch.tensor(ln, dtype=torch.int32)), slots.copy_(torch.tensor(sl, dtype=torch.int32))
+        win.copy_(win0), h.copy_(h0)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = calls(win0.clone(), h0.clone())
+        torch.cuda.synchronize()
+        for k, (a, b) in enumerate(zip(captured, eager)):
+            assert torch.equal(a, b), (ln, sl, k)
+
+
+def test_inputs_that_share_memory():
+    """Inputs repeated over sequences, tokens or groups by strides of zero."""
+    N, L, C, S, G = 3, 21, 66, 8, 2
+    x, st, dout, _ = _inputs(22, torch.float32, N, L, C, S, G)
+    x["delta"] = x["delta"][:, :1].expand(N, L, C)
+    x["z"] = x["z"][:1].expand(N, L, C)
+    x["B"] = x["B"][:, :, :1].expand(N, L, G, S)
+    x["C"] = x["C"][:1, :1].expand(N, L, G, S)
+    dout = dout[:1].expand(N, L, C)
+    full = {k: t if t is None else t.contiguous() for k, t in x.items()}
+    assert torch.equal(dconv.dconv_scan(**x, state=st), dconv.dconv_scan(**full, state=st))
+    for a, b in zip(dconv.dconv_scan_grad(dout, **x, state=st), dconv.dconv_scan_grad(dout.contiguous(), **full, state=st)):
+        assert torch.equal(a, b)
+
+
+def test_two_threads_on_streams_of_their_own():
+    import threading
+    x, st, dout, _ = _inputs(23, torch.bfloat16, 1, 300, 72, 16, 1)
+    want, grads = dconv.dconv_scan(**x, state=st), dconv.dconv_scan_grad(dout, **x, state=st)
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work():
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                a, b = dconv.dconv_scan(**x, state=st), dconv.dconv_scan_grad(dout, **x, state=st)
+            s.synchronize()
+            if not (torch.equal(a, want) and all(torch.equal(p, q) for p, q in zip(b, grads))):
+                wrong.append(1)
+
+    threads = [threading.Thread(target=work) for _ in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong

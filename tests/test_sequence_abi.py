@@ -69,6 +69,7 @@ def test_causal_refusals(name):
             assert causal(name, **{k: v}) == SHAPE, k
     assert causal(name, F=9) == SHAPE
     assert causal(name, L=(1 << 30) + 1) == SHAPE
+    assert causal(name, N=1, C=(1 << 30) + 1) == SHAPE
     assert causal(name, N=2147483647, C=2147483647, M=2147483647) == SHAPE           # more workgroups than a launch has
     for d in (2, 4, -1):
         assert causal(name, dtype=d) == UNSUPPORTED
@@ -105,6 +106,7 @@ def test_scan_refusals(name):
     assert scan(name, S=33) == SHAPE
     assert scan(name, G=3) == SHAPE                                            # 70 channels in 3 groups
     assert scan(name, L=(1 << 30) + 1) == SHAPE
+    assert scan(name, N=1, C=(1 << 30) + 1) == SHAPE
     assert scan(name, N=1 << 30, C=1 << 30, M=1 << 30) == SHAPE
     for d in (2, 4, -1):
         assert scan(name, dtype=d) == UNSUPPORTED
