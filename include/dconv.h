@@ -508,9 +508,10 @@ typedef struct dconv_scan_args {
 int dconv_scan(const dconv_scan_args *a, void *stream);
 int dconv_scan_grad(const dconv_scan_args *a, void *stream);
 int dconv_scan_step(const dconv_scan_args *a, void *stream);
-/* Bytes of workspace for dconv_scan (grad == 0; 0 bytes for some) or dconv_scan_grad
- * (looks at the sizes, dtype and whether starts is NULL), and of `starts`; -1 where
- * the sizes are not valid.  Host arithmetic. */
+/* Bytes of workspace for dconv_scan (grad == 0; none for some short calls with
+ * outputs) or dconv_scan_grad (looks at the sizes, dtype and whether out.p and
+ * starts are NULL), and of `starts`; -1 where the sizes are not valid.  Host
+ * arithmetic. */
 long long dconv_scan_workspace(const dconv_scan_args *a, int grad);
 long long dconv_scan_starts(const dconv_scan_args *a);
 

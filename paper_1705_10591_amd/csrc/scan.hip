@@ -29,13 +29,15 @@ bc_kernel(Rows B, Rows C, int64_t b_g, int64_t c_g, const int* lengths, float* b
 // OUT: the outputs of all tokens, with the states wanted on the way; otherwise the states alone, and with `ends` those of each chunk
 // begun at zero (the first at the call's state, which is kept for the second launch in the last chunk's place).
 // WHOLE: the block has 64 channels, so that no run of them is cut.
-template <int W, bool OUT> struct ScanLds {
+// SHORT: B and C by way of LDS.
+template <int W, bool OUT, bool SHORT> struct ScanLds {
     float2 step[kT][kWave];                             // d, d u
     float ysum[OUT ? W : 1][kT][kWave];
+    f8 bc[SHORT ? W : 1][kT];                           // as in memory
 };
 
-template <typename T, int W, int R, bool OUT, bool WHOLE>
-__device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace& a, ScanLds<W, OUT>& lds, bool ends)
+template <typename T, int W, int R, bool OUT, bool SHORT, bool WHOLE>
+__device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace& a, ScanLds<W, OUT, SHORT>& lds, bool ends)
 {
     constexpr int E = kT / W;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -80,7 +82,18 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
     Share<T, E> po(p.out, a.n, t, ec);
     pu.spare(); pd.spare(); pz.spare(); po.spare();
     Run<T, E> u{}, dl{}, z{}, ul{}, zl{};                 // of the tile fetched, the one at hand
+    // SHORT: B and C of a token and wave by each of the first 16 W threads
+    const int bt = tid / W, bw = tid % W, bs = min(R, p.S - bw * R);
+    Run<T, R> rb{}, rc{};
     auto fetch = [&](int at) {
+        if constexpr (SHORT) {
+            const int tok = at - tt + bt;
+            rb = rc = Run<T, R>{};
+            if (bt < kT && tok < a.len) {
+                rb = load_some<R>(p.B.at<const T>(a.n, tok, bw * R) + a.g * p.b_g, bs);
+                if (OUT) rc = load_some<R>(p.Cm.at<const T>(a.n, tok, bw * R) + a.g * p.c_g, bs);
+            }
+        }
         if (at < a.len && nv > 0) {
             u = pu.load(nv);
             dl = pd.load(nv);
@@ -104,6 +117,16 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
         }
 #pragma unroll
         for (int i = 0; i < E; ++i) lds.step[tt][tc + i] = make_float2(d_[i], d_[i] * u_[i]);
+        if constexpr (SHORT) {
+            if (bt < kT) {
+                float* to = (float*)&lds.bc[bw][bt & ~1] + (bt & 1) * kR;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    to[r] = rb[r];
+                    if (OUT) to[2 * kR + r] = rc[r];
+                }
+            }
+        }
     };
     auto finish = [&](int tile, int at) {                 // the tile at hand: sums over waves, gate
         if (nv > 0 && at < p.L) {
@@ -133,7 +156,7 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
     BC<OUT> bc, next;
     if (a.tile0 < a.stop) {
         fetch(t);
-        bc.load(bc_of(p, a, a.tile0, W, wave));
+        if (!SHORT) bc.load(bc_of(p, a, a.tile0, W, wave));
     }
     for (int tile = a.tile0; tile < a.stop; ++tile, t += kT) {
         const auto& step = lds.step;
@@ -147,12 +170,15 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
         float ys[kStep];
 #pragma unroll
         for (int k = 0; k < kStep; ++k) d[k] = step[k][lane];
-        const bc_ptr here = bc_of(p, a, tile, W, wave), after = bc_of(p, a, min(tile + 1, a.stop - 1), W, wave);
+        const bc_ptr here = SHORT ? nullptr : bc_of(p, a, tile, W, wave);
+        const bc_ptr after = SHORT ? nullptr : bc_of(p, a, min(tile + 1, a.stop - 1), W, wave);
+        if (SHORT) bc.load(&lds.bc[wave][0]);
 #pragma unroll
         for (int k0 = 0; k0 < kT; k0 += kStep) {
             const bool more = k0 + kStep < kT;
             arrived();
-            next.load(more ? here + k0 + kStep : after);
+            if (!SHORT) next.load(more ? here + k0 + kStep : after);
+            else if (more) next.load(&lds.bc[wave][k0 + kStep]);
 #pragma unroll
             for (int k = 0; k < kStep; ++k) {
                 if (more) dn[k] = step[k0 + kStep + k][lane];
@@ -195,22 +221,23 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
     }
 }
 
-template <typename T, int W, int R, bool OUT>
+template <typename T, int W, int R, bool OUT, bool SHORT>
 __global__ void __launch_bounds__(kWave * W)
 scan_kernel(ScanParams p, bool ends)
 {
-    __shared__ ScanLds<W, OUT> lds;
+    __shared__ ScanLds<W, OUT, SHORT> lds;
     const ScanPlace a = scan_place(p);
-    if (a.nc == kWave) scan_block<T, W, R, OUT, true>(p, a, lds, ends);
-    else scan_block<T, W, R, OUT, false>(p, a, lds, ends);
+    if (a.nc == kWave) scan_block<T, W, R, OUT, SHORT, true>(p, a, lds, ends);
+    else scan_block<T, W, R, OUT, SHORT, false>(p, a, lds, ends);
 }
 
 template <typename T, int W, int R>
 void launch_kernel(const ScanParams& p, bool out, bool ends, int64_t blocks, hipStream_t st)
 {
     const dim3 grid((unsigned)blocks), threads(kWave * W);
-    if (out) hipLaunchKernelGGL((scan_kernel<T, W, R, true>), grid, threads, 0, st, p, false);
-    else hipLaunchKernelGGL((scan_kernel<T, W, R, false>), grid, threads, 0, st, p, ends);
+    if (!p.bc) hipLaunchKernelGGL((scan_kernel<T, W, R, true, true>), grid, threads, 0, st, p, false);
+    else if (out) hipLaunchKernelGGL((scan_kernel<T, W, R, true, false>), grid, threads, 0, st, p, false);
+    else hipLaunchKernelGGL((scan_kernel<T, W, R, false, false>), grid, threads, 0, st, p, ends);
 }
 
 template <typename T>
@@ -280,6 +307,14 @@ ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
     return pl;
 }
 
+// Short calls: up to six tiles where the chip has at most two waves a SIMD.  Measured, us a call without and with
+// (sequences x tokens x channels, 16 states): 1 x 16 x 2048 20, 16.5; 1 x 64 x 2048 20, 17; 8 x 64 x 4096 20.3, 19.2;
+// 32 x 64 x 4096 43, 47; 8 x 256 x 4096 47, 49.5; 8 x 1024 x 4096 163, 176.
+bool scan_short(const dconv_scan_args& a, const ScanPlan& pl)
+{
+    return a.out.p && pl.chunks == 1 && pl.tiles <= 6 && (double)a.N * pl.blocks * pl.waves <= 2048;
+}
+
 int64_t scan_bc_floats(const dconv_scan_args& a, const ScanPlan& pl)
 {
     return (int64_t)a.N * a.G * pl.tiles * kT * pl.waves * 2 * kR;
@@ -303,6 +338,7 @@ ScanParams scan_params(const dconv_scan_args& a, const ScanPlan& pl)
     p.dout = rows_of(a.dout); p.du = rows_of(a.du); p.ddelta = rows_of(a.ddelta); p.dz = rows_of(a.dz);
     p.A = a.A; p.D = a.D; p.delta_bias = a.delta_bias; p.state = a.state; p.dstate_out = a.dstate_out;
     p.state_out = a.state_out; p.dstate = a.dstate; p.starts = (float*)a.starts;
+    p.B = rows_of(a.B); p.Cm = rows_of(a.Cm); p.b_g = a.B.sg; p.c_g = a.Cm.sg;
     p.lengths = a.lengths;
     p.N = a.N; p.L = a.L; p.C = a.C; p.S = a.S; p.G = a.G; p.softplus = a.softplus;
     p.group = pl.group; p.gblocks = pl.gblocks; p.blocks = pl.blocks;
@@ -360,10 +396,11 @@ int scan_check(const dconv_scan_args* a, int form)
                           (const void*)a->dD, (const void*)a->ddelta_bias, (const void*)a->starts, (const void*)a->lengths,
                           (const void*)a->slots})
         if (!aligned_to(q, 4)) return DCONV_BAD_SHAPE;
-    if (!step) {
+    const long long need = step ? 0 : dconv_scan_workspace(a, grad);
+    if (need) {
         if (!a->workspace) return DCONV_NULL_POINTER;
         if (!aligned_to(a->workspace, 16)) return DCONV_BAD_SHAPE;
-        if (a->workspace_bytes < dconv_scan_workspace(a, grad)) return DCONV_SCRATCH_EXCEEDED;
+        if (a->workspace_bytes < need) return DCONV_SCRATCH_EXCEEDED;
     }
     return DCONV_OK;
 }
@@ -386,6 +423,7 @@ int dconv_scan(const dconv_scan_args* a, void* stream)
     const ScanPlan pl = scan_plan(*a, false);
     ScanParams p = scan_params(*a, pl);
     float* ws = (float*)a->workspace;
+    if (scan_short(*a, pl)) return launch_scan_forward(*a, p, pl, true, (hipStream_t)stream);
     p.bc = ws;
     p.ends = ws + scan_bc_floats(*a, pl);
     p.dsum = p.ends + (int64_t)a->N * pl.chunks * pl.blocks * pl.waves * kWave * pl.states;

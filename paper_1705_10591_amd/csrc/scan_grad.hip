@@ -697,6 +697,7 @@ long long dconv_scan_workspace(const dconv_scan_args* a, int grad)
 {
     if (!a || !token_bytes(a->dtype) || !scan_sizes_ok(*a)) return -1;
     const ScanPlan pl = scan_plan(*a, grad != 0);
+    if (!grad && scan_short(*a, pl)) return 0;
     return 4 * (grad ? space_of(*a, pl).all : scan_bc_floats(*a, pl) + scan_chunk_floats(*a, pl));
 }
 

@@ -14,6 +14,9 @@
 //  * Scalar loads come back in any order, so that a wait for one is a wait for all: a tile is walked in steps of kStep = 4
 //    tokens.  A step waits for its operands, asks for those of the next one (64 of B and C in scalar registers, d and d u from
 //    LDS), writes the sums of the last one, and calculates.
+//    A short call (a few tiles, no chunks) would wait for that kernel longer than it takes itself: its workgroups lay a tile's B
+//    and C out in LDS and read them from there, 16 bytes a lane that are the same for all.  LDS has time for that
+//    only where the vector ALU has gaps.
 //  * A call with too few (sequence, channel block) pairs for the chip cuts its sequences into chunks: a first launch
 //    runs each chunk from a state of zero, and each workgroup of the second begins by putting together what the chunks
 //    before it leave, since a chunk changes the state it is given by the factor exp(A sum d) alone.
@@ -37,7 +40,7 @@ typedef const __attribute__((address_space(4))) f8* bc_ptr;        // constant m
 // B of kStep tokens, and C where it is needed (WITH_C): pairs of tokens, four states each.
 template <bool WITH_C> struct BC {
     f8 vb[kStep / 2], vc[WITH_C ? kStep / 2 : 1];
-    __device__ __forceinline__ void load(bc_ptr p)
+    template <typename P> __device__ __forceinline__ void load(P p)              // bc_ptr, or const f8* in LDS
     {
 #pragma unroll
         for (int i = 0; i < kStep / 2; ++i) {
@@ -59,7 +62,8 @@ struct Rows {                        // a token tensor: base, elements between s
 };
 
 struct ScanParams {
-    Rows u, delta, z, out, dout, du, ddelta, dz;
+    Rows u, delta, z, out, dout, du, ddelta, dz, B, Cm;
+    int64_t b_g, c_g;                // elements between groups of B and C
     const float *A, *D, *delta_bias, *state, *dstate_out;
     float *state_out, *dstate, *starts;
     const int* lengths;
@@ -183,6 +187,7 @@ int scan_check(const dconv_scan_args* a, int form);        // 0 prompt, 1 gradie
 struct ScanPlan { int waves, states, group, gblocks, blocks, tiles, chunks, chunk_tiles; };
 ScanPlan scan_plan(const dconv_scan_args& a, bool grad);
 ScanParams scan_params(const dconv_scan_args& a, const ScanPlan& pl);
+bool scan_short(const dconv_scan_args& a, const ScanPlan& pl);
 int64_t scan_bc_floats(const dconv_scan_args& a, const ScanPlan& pl);
 int64_t scan_chunk_floats(const dconv_scan_args& a, const ScanPlan& pl);      // ends and dsum
 int64_t scan_starts_floats(const dconv_scan_args& a);

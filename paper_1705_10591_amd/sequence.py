@@ -153,7 +153,8 @@ def _causal_bytes(code, N, L, C, F):
 @lru_cache(maxsize=4096)
 def _scan_bytes(code, N, L, C, S, G, form):
     """Of the workspace of a prompt ("scan"), a gradient with and without starts ("grad", "starts grad"), of the starts."""
-    args = _SCAN.pack(code, N, L, C, S, G, 0, 0, *(12 * _NONE), *(10 * (0,)), 16 if form == "starts grad" else 0, 0, 0, 0, 0)
+    tokens = (*(3 * _NONE), 16, 0, 0, 0, *(8 * _NONE))               # (a prompt that has an output)
+    args = _SCAN.pack(code, N, L, C, S, G, 0, 0, *tokens, *(10 * (0,)), 16 if form == "starts grad" else 0, 0, 0, 0, 0)
     if form == "starts":
         return _lib().dconv_scan_starts(args)
     return _lib().dconv_scan_workspace(args, 0 if form == "scan" else 1)
@@ -328,13 +329,14 @@ def dconv_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.T
         _fits(out, wide, dtype, index, "out")
         _apart(out, "out")
     need = _scan_bytes(code, N, L, ch, S, G, "scan")
-    ws = _workspace(need, u)
+    ws = _workspace(need, u) if need else None
     _run(_lib().dconv_scan, index, _SCAN.pack(
             code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
             *_rows(out, wide, dtype, index, "out"), *bc[0], *bc[1], *(6 * _NONE), *params,
             _dense(state, (N, ch, S), torch.float32, index, "state"),
             _dense(state_out, (N, ch, S), torch.float32, index, "state_out"), 0, 0, 0, 0, 0,
-            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"), 0, ws.data_ptr(), need))
+            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"), 0,
+            0 if ws is None else ws.data_ptr(), need))
     return out
 
 

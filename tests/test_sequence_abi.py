@@ -32,7 +32,7 @@ def causal(name, **change):
 
 
 def scan(name, **change):
-    v = {"dtype": 1, "N": 2, "L": 1 if name.endswith("step") else 9, "C": 70, "S": 16, "G": 1, "M": 2, "softplus": 1, "A": P, "state_out": P,
+    v = {"dtype": 1, "N": 2, "L": 1 if name.endswith("step") else 200, "C": 70, "S": 16, "G": 1, "M": 2, "softplus": 1, "A": P, "state_out": P,
          "dA": P, "workspace": P, "workspace_bytes": 1 << 50}
     v.update({t + ".p": P for t in ("u", "delta", "out", "B", "Cm", "dout", "du", "ddelta", "dB", "dC")})
     v.update({k.replace("_p", ".p") if k.endswith("_p") else k: t for k, t in change.items()})
@@ -121,7 +121,7 @@ def test_scan_refusals(name):
         assert scan(name, M=0, slots=P) == SHAPE
     else:
         lib = dconv.load_library()
-        sizes = _pack(SCAN, q._SCAN, {"dtype": 1, "N": 2, "L": 9, "C": 70, "S": 16, "G": 1})
+        sizes = _pack(SCAN, q._SCAN, {"dtype": 1, "N": 2, "L": 200, "C": 70, "S": 16, "G": 1, "out.p": P})
         need = lib.dconv_scan_workspace(sizes, int(grad))
         assert need > 0 and scan(name, workspace_bytes=need - 1) == SCRATCH
         assert scan(name, workspace=P + 8) == SHAPE
@@ -133,6 +133,10 @@ def test_sizes_of_workspaces():
     assert lib.dconv_scan_workspace(bad, 0) == lib.dconv_scan_workspace(bad, 1) == lib.dconv_scan_starts(bad) == -1
     assert lib.dconv_causal_workspace(_pack(CAUSAL, q._CAUSAL, {"dtype": 1, "N": 1, "L": 1, "C": 1, "F": 9})) == -1
     assert lib.dconv_scan_starts(None) == lib.dconv_scan_workspace(None, 1) == lib.dconv_causal_workspace(None) == -1
+    # a short prompt needs none for its output, but for the states alone
+    short = {"dtype": 1, "N": 2, "L": 9, "C": 70, "S": 16, "G": 1}
+    assert lib.dconv_scan_workspace(_pack(SCAN, q._SCAN, {**short, "out.p": P}), 0) == 0
+    assert lib.dconv_scan_workspace(_pack(SCAN, q._SCAN, short), 0) > 0
     # sizes that pass 32 bits
     big = _pack(SCAN, q._SCAN, {"dtype": 1, "N": 64, "L": 1 << 17, "C": 8192, "S": 16, "G": 1})
     assert lib.dconv_scan_starts(big) == 64 * (1 << 13) * 8192 * 16 * 4
