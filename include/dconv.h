@@ -415,7 +415,9 @@ int dconv_general_noalloc(const float *in, int N, int C, int H, int W,
  *     row whose slot is not in 0..M-1, or is that of an earlier row, is padding: its
  *     outputs are written as 0 and no state is touched.
  *   - The state that a prompt leaves may be written over the one that it read
- *     (state_out == state); apart from that outputs must not overlap inputs.
+ *     (state_out == state); apart from that outputs must not overlap inputs (a
+ *     convolution's output or dx at the address of an input is refused with
+ *     DCONV_BAD_SHAPE).
  *   - Nothing is allocated, no call synchronises, results are the same bits on
  *     every call, and all calls may be captured.  What a call needs between its
  *     kernels lies in the caller's workspace (16-byte aligned; sizes from
@@ -424,8 +426,8 @@ int dconv_general_noalloc(const float *in, int N, int C, int H, int W,
  *     graphs among them, need one each.
  *   - Errors: a required pointer (or the argument struct) that is NULL ->
  *     DCONV_NULL_POINTER; a size <= 0, F > 8, S > 32, C not a multiple of G, more
- *     than 2^30 channels or tokens of a sequence, work beyond 2^31-1 workgroups, misaligned
- *     data -> DCONV_BAD_SHAPE; another element type -> DCONV_UNSUPPORTED; a workspace that
+ *     than 2^30 channels or tokens of a sequence, more work than a launch of 2^32
+ *     threads holds, misaligned data -> DCONV_BAD_SHAPE; another element type -> DCONV_UNSUPPORTED; a workspace that
  *     is too small -> DCONV_SCRATCH_EXCEEDED.
  */
 typedef struct dconv_tokens {
@@ -475,7 +477,7 @@ long long dconv_causal_workspace(const dconv_causal_args *a);
  *   out = y * z * sigmoid(z) with a gate z, y without
  * h before token 0 is state [N][C][S] (NULL: zeros), h behind the sequence's end
  * goes to state_out (NULL: not wanted).  `starts` (NULL: not wanted) keeps states
- * on the way, dconv_scan_starts bytes of the library's own layout, from which
+ * on the way, dconv_scan_starts bytes (16-byte aligned) of the library's own layout, from which
  * dconv_scan_grad goes back; with out.p NULL only starts and state_out are made
  * (Cm, D and z are not read then).
  * dconv_scan_grad: from dout the gradients of all inputs; dstate_out is the

@@ -218,7 +218,7 @@ __device__ __forceinline__ void causal_grad_strip(const CausalParams& p, Place a
                 }
                 d = t < len ? d : 0.f;
                 ds[F - 1][i] = d;
-                if (t < end) {
+                if (t < min(end, len)) {             // (not 0 times what stands before a sequence without tokens)
 #pragma unroll
                     for (int j = 0; j < F; ++j) acc[j][i] = __builtin_fmaf(d, rows[j][i], acc[j][i]);
                     acc[F][i] += d;
@@ -334,7 +334,6 @@ causal_step_kernel(CausalParams p)
 // ---- host ------------------------------------------------------------------------------------------------------------
 
 constexpr int kMaxTaps = 8;
-constexpr int64_t kMaxBlocks = 2147483647LL;
 
 bool sizes_ok(const dconv_causal_args& a)
 {
@@ -369,6 +368,8 @@ int check(const dconv_causal_args* a, bool step, bool grad)
     if (!sizes_ok(*a) || (step && (a->L != 1 || a->M <= 0 || (!a->slots && a->M < a->N)))) return DCONV_BAD_SHAPE;
     if (!a->x.p || !a->filt || (!grad && !a->out.p) || (grad && (!a->dout.p || !a->dx.p))) return DCONV_NULL_POINTER;
     if (step && a->F > 1 && !a->state_out) return DCONV_NULL_POINTER;
+    // (rows are read by the strips on both sides of them)
+    if (!step && (grad ? a->dx.p == a->x.p || a->dx.p == a->dout.p : a->out.p == a->x.p)) return DCONV_BAD_SHAPE;
     for (const void* q : {(const void*)a->x.p, (const void*)a->out.p, (const void*)a->dout.p, (const void*)a->dx.p, a->filt,
                           a->bias, a->state, (const void*)a->state_out, a->dstate_out, (const void*)a->dstate})
         if (!aligned_to(q, e)) return DCONV_BAD_SHAPE;
@@ -394,7 +395,7 @@ enum class Form { kPrompt, kGrad, kStep };
 template <typename T, int F> int launch(Form form, const CausalParams& p, hipStream_t st)
 {
     constexpr int V = 16 / sizeof(T), VG = 4;
-    if (p.total > kMaxBlocks) return DCONV_BAD_SHAPE;
+    if (p.total > kMaxThreads / kThreads) return DCONV_BAD_SHAPE;
     const dim3 grid((unsigned)p.total);
     begin_launch();
     switch (form) {

@@ -272,10 +272,11 @@ bool scan_sizes_ok(const dconv_scan_args& a)
     // (sizes in floating point, so that no product overflows)
     if ((double)a.N * a.L * a.C * kMaxStates >= kMaxElements) return false;
     const ScanPlan pl = scan_plan(a, false);             // (a gradient has no more chunks)
-    // (workgroups of the largest grids: the scans', bc_kernel's, the sums')
+    // (threads of the largest grids: the scans', bc_kernel's, the sums')
     const double bc = (double)a.N * a.G * pl.tiles * pl.waves;
-    return (double)a.N * pl.blocks * pl.chunks <= 2147483647.0 && bc * kT / kThreads <= 2147483646.0 &&
-           bc * (kT / 8 * kWave) / kThreads + pl.blocks * (kMaxStates + 2.0) <= 2147483646.0;
+    const double most = (double)kMaxThreads - kThreads;
+    return (double)a.N * pl.blocks * pl.chunks * pl.waves * kWave <= most && bc * kT <= most &&
+           bc * (kT / 8 * kWave) + pl.blocks * (kMaxStates + 2.0) * kThreads <= most;
 }
 
 ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
@@ -393,9 +394,10 @@ int scan_check(const dconv_scan_args* a, int form)
         if (!aligned_to(t->p, e)) return DCONV_BAD_SHAPE;
     for (const void* q : {(const void*)a->A, (const void*)a->D, (const void*)a->delta_bias, (const void*)a->state,
                           (const void*)a->state_out, (const void*)a->dstate_out, (const void*)a->dstate, (const void*)a->dA,
-                          (const void*)a->dD, (const void*)a->ddelta_bias, (const void*)a->starts, (const void*)a->lengths,
+                          (const void*)a->dD, (const void*)a->ddelta_bias, (const void*)a->lengths,
                           (const void*)a->slots})
         if (!aligned_to(q, 4)) return DCONV_BAD_SHAPE;
+    if (!step && !aligned_to(a->starts, 16)) return DCONV_BAD_SHAPE;
     const long long need = step ? 0 : dconv_scan_workspace(a, grad);
     if (need) {
         if (!a->workspace) return DCONV_NULL_POINTER;

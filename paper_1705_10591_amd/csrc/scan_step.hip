@@ -92,7 +92,7 @@ extern "C" int dconv_scan_step(const dconv_scan_args* a, void* stream)
     const int W = a->S <= 4 ? 1 : a->S <= 8 ? 2 : a->S <= 16 ? 4 : 8;
     p.cblocks = (a->C - 1) / (kThreads / W) + 1;
     const int64_t blocks = (int64_t)a->N * p.cblocks;
-    if (blocks > 2147483647LL) return DCONV_BAD_SHAPE;
+    if (blocks > kMaxThreads / kThreads) return DCONV_BAD_SHAPE;
     const hipStream_t st = (hipStream_t)stream;
     begin_launch();
     if (a->dtype == DCONV_DTYPE_F16) launch_typed<_Float16>(p, W, blocks, st);

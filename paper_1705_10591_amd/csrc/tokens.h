@@ -70,6 +70,7 @@ __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts
 
 constexpr int kMaxTokens = 1 << 30;      // of a sequence: token numbers and what is added to them fit 32 bits
 constexpr int kMaxChannels = 1 << 30;    // likewise
+constexpr int64_t kMaxThreads = 4294967295LL;   // of a launch: a packet holds 32 bits of them
 constexpr double kMaxElements = 1.1e18;  // of a tensor, 2^60: sizes in 64 bits do not overflow
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;

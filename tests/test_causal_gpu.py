@@ -144,6 +144,17 @@ def test_steps(N, C, F, dtype):
     assert torch.equal(dconv.dconv_causal_step(x[:, 0], plain, w, b)[live], whole[live, 0])
 
 
+def test_a_sequence_without_tokens_adds_nothing_whatever_its_state_holds():
+    N, L, C, F = 2, 20, 16, 4
+    x, w, b, st, dout, dlast = _inputs(7, torch.float32, N, L, C, F)
+    lengths = torch.tensor([20, 0], dtype=torch.int32, device="cuda")
+    st[1], x[1], dout[1] = NAN, NAN, NAN
+    got = dconv.dconv_causal_grad(dout, x, w, b, state=st, lengths=lengths, dstate_out=dlast)
+    one = dconv.dconv_causal_grad(dout[:1], x[:1], w, b, state=st[:1], dstate_out=dlast[:1])
+    assert torch.equal(got.dfilt, one.dfilt) and torch.equal(got.dbias, one.dbias)
+    assert torch.equal(got.dx[0], one.dx[0]) and not got.dx[1].any() and torch.equal(got.dstate[1], dlast[1])
+
+
 def test_rows_beyond_32_bits():
     """Tokens whose elements lie more than 2^31 (and 2^32 bytes) from the first."""
     N, L, C, F = 2, 3, 64, 4

@@ -25,8 +25,8 @@ def _pack(names, layout, values):
 
 
 def causal(name, **change):
-    v = {"dtype": 1, "N": 2, "L": 1 if name.endswith("step") else 9, "C": 70, "F": 4, "M": 2, "silu": 1, "x.p": P, "out.p": P,
-         "dout.p": P, "dx.p": P, "filt": P, "state_out": P, "dfilt": P, "workspace": P, "workspace_bytes": 1 << 40}
+    v = {"dtype": 1, "N": 2, "L": 1 if name.endswith("step") else 9, "C": 70, "F": 4, "M": 2, "silu": 1, "x.p": P, "out.p": P + 16,
+         "dout.p": P, "dx.p": P + 16, "filt": P, "state_out": P, "dfilt": P, "workspace": P, "workspace_bytes": 1 << 40}
     v.update({k.replace("_p", ".p") if k in ("x_p", "out_p", "dout_p", "dx_p") else k: t for k, t in change.items()})
     return getattr(dconv.load_library(), name)(_pack(CAUSAL, q._CAUSAL, v), None)
 
@@ -78,6 +78,8 @@ def test_causal_refusals(name):
             assert causal(name, **{k: P + 1}) == SHAPE, k
     assert causal(name, dtype=3, x_p=P + 2) == SHAPE
     assert causal(name, lengths=P + 2) == SHAPE
+    if not step:
+        assert causal(name, **{"dx_p" if grad else "out_p": P}) == SHAPE       # over x
     if step:
         assert causal(name, L=2) == SHAPE
         assert causal(name, M=1) == SHAPE                    # fewer windows than rows, no slots
@@ -113,7 +115,7 @@ def test_scan_refusals(name):
     for k in needed:
         assert scan(name, **{k: P + 1}) == SHAPE, k
     assert scan(name, dtype=3, u_p=P + 2) == SHAPE
-    for k in ("D", "delta_bias", "state", "lengths", "slots", "starts"):
+    for k in ("D", "delta_bias", "state", "lengths", "slots"):
         assert scan(name, **{k: P + 2}) == SHAPE, k
     if step:
         assert scan(name, L=2) == SHAPE
@@ -125,6 +127,7 @@ def test_scan_refusals(name):
         need = lib.dconv_scan_workspace(sizes, int(grad))
         assert need > 0 and scan(name, workspace_bytes=need - 1) == SCRATCH
         assert scan(name, workspace=P + 8) == SHAPE
+        assert scan(name, starts=P + 8) == SHAPE
 
 
 def test_sizes_of_workspaces():
