@@ -21,13 +21,17 @@ DTYPE_F32 = 3
 _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: DTYPE_F32}
 
 # The argument structs of dconv.h, packed at once: filling a ctypes structure field by field takes several times as long
-# as a single token takes the GPU.
+# as a single token takes the GPU.  A token tensor is four fields: pointer, strides of sequence, token and group.
 _CAUSAL = struct.Struct("8i" + 4 * "4q" + "12q")
 _SCAN = struct.Struct("8i" + 12 * "4q" + "15q")
-# ... of the step forms, which leave most fields empty
-_CAUSAL_STEP = struct.Struct("8i" + "qq16x" * 2 + "64x" + "qq8xq40xq16x")
-_SCAN_STEP = struct.Struct("8i" + "qq16x" * 4 + "qq8xq" * 2 + "192x" + "qqq8xq56xq16x")
-_NONE = (0, 0, 0, 0)
+# ... of each form, without the fields that it leaves empty
+_CAUSAL_PROMPT = struct.Struct("8i" + 2 * "3q8x" + "64x" + "4q" + "32x" + "q" + "24x")
+_CAUSAL_GRAD = struct.Struct("8i" + "3q8x" + "32x" + 2 * "3q8x" + "3q8x" + "4q" + "q8x" + "2q")
+_CAUSAL_STEP = struct.Struct("8i" + 2 * "2q16x" + "64x" + "2q8xq40xq16x")
+_SCAN_PROMPT = struct.Struct("8i" + 4 * "3q8x" + 2 * "4q" + "192x" + "5q" + "40x" + "2q8x" + "2q")
+_SCAN_GRAD = struct.Struct("8i" + 3 * "3q8x" + "32x" + 2 * "4q" + 4 * "3q8x" + 2 * "4q" + "4q8x" + "5q" + "2q8x" + "2q")
+_SCAN_STEP = struct.Struct("8i" + 4 * "2q16x" + 2 * "2q8xq" + "192x" + "3q8xq56xq16x")
+_NONE, _NONE3 = (0, 0, 0, 0), (0, 0, 0)
 _INT32, _FLOAT32 = torch.int32, torch.float32
 # (torch.cuda.current_device and a Stream object take as long as all checks of a call)
 _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
@@ -44,13 +48,14 @@ def declare(lib: ctypes.CDLL) -> None:
             fn.restype = ctypes.c_int
 
 
-_loaded = _package = None
+_loaded = _package = _raw_stream = None
 
 
 def _lib():
-    global _loaded, _package
+    global _loaded, _package, _raw_stream
     if _loaded is None:
         _package = sys.modules[__package__]
+        _raw_stream = _package._raw_stream
         _loaded = _package.load_library()
     return _loaded
 
@@ -58,23 +63,24 @@ def _lib():
 def _run(fn, index, args):
     if index != _device():
         return _package._enqueue(fn, index, args)
-    rc = fn(args, _package._raw_stream(index))
+    rc = fn(args, _raw_stream(index))
     if rc:
         _package._raise(rc)
 
 
-def _bad_shape():
-    _lib()
-    _package._raise(_package.STATUS_BAD_SHAPE)
-
+# One token of one row takes the GPU 2.4 us and the host three times as long, most of it in the checks below: a tensor that
+# fits is looked at in one expression, and what does not fit is looked into afterwards.  (Sizes of zero are the library's to refuse.)
 
 def _first(t, dims, what):
-    """Type, its number, and device that the other tensors of a call have to agree with."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _DTYPES and t.dim() == dims):
-        raise TypeError(f"{what} must be a float16, bfloat16 or float32 CUDA tensor with {dims} dims")
-    if 0 in t.shape:
-        _bad_shape()
-    return t.dtype, _DTYPES[t.dtype], t.get_device()
+    """Type, its number, device and shape that the other tensors of a call have to agree with."""
+    try:
+        dtype, shape = t.dtype, t.shape
+        code, index = _DTYPES.get(dtype), t.get_device()
+        if code is not None and index >= 0 and len(shape) == dims:
+            return dtype, code, index, shape
+    except AttributeError:
+        pass
+    raise TypeError(f"{what} must be a float16, bfloat16 or float32 CUDA tensor with {dims} dims")
 
 
 def _refuse(t, shape, dtype, index, what):
@@ -83,13 +89,18 @@ def _refuse(t, shape, dtype, index, what):
         raise TypeError(f"{what} must be a CUDA tensor of type {dtype}")
     if t.get_device() != index:
         raise ValueError(f"{what} is on another device")
-    raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    raise TypeError(f"{what} must be contiguous")
 
 
-def _fits(t, shape, dtype, index, what):
+def _strides(t, shape, dtype, index, what):
     try:
         if t.dtype is dtype and t.get_device() == index and t.shape == shape:
-            return
+            s = t.stride()
+            if s[-1] == 1 or shape[-1] == 1:
+                return s
+            raise TypeError(f"the last dimension of {what} must be contiguous")
     except AttributeError:
         pass
     _refuse(t, shape, dtype, index, what)
@@ -97,41 +108,47 @@ def _fits(t, shape, dtype, index, what):
 
 def _row(t, shape, dtype, index, what):
     """(pointer, stride) of the rows of a step's token tensor."""
-    _fits(t, shape, dtype, index, what)
-    s = t.stride()
-    if s[1] != 1 and shape[1] != 1:
-        raise TypeError(f"the last dimension of {what} must be contiguous")
+    s = _strides(t, shape, dtype, index, what)
     return t.data_ptr(), s[0]
 
 
 def _rows(t, shape, dtype, index, what):
-    """(pointer, strides of sequence, token and group) of a token tensor."""
+    """(pointer, strides of sequence and token) of a token tensor."""
+    if t is None:
+        return _NONE3
+    s = _strides(t, shape, dtype, index, what)
+    return t.data_ptr(), s[0], s[1]
+
+
+def _groups(t, shape, dtype, index, what):
+    """(pointer, strides of sequence, token and group) of B, C and their gradients."""
     if t is None:
         return _NONE
-    _fits(t, shape, dtype, index, what)
-    s = t.stride()
-    if s[-1] != 1 and shape[-1] != 1:
-        raise TypeError(f"the last dimension of {what} must be contiguous")
-    return (t.data_ptr(), s[0], s[1], s[2] if len(s) == 4 else 0)
+    s = _strides(t, shape, dtype, index, what)
+    return t.data_ptr(), s[0], s[1], s[2]
 
 
-def _apart(t, what):
-    """Refuses an output whose tokens share memory: they would be written by several workgroups."""
-    span = t.shape[-1]
-    for stride, size in sorted(zip(t.stride()[:-1], t.shape[:-1])):
+def _output(t, shape, dtype, index, what):
+    """_rows of an output that the caller gives.  Tokens that share memory would be written by several workgroups."""
+    s = _strides(t, shape, dtype, index, what)
+    span = shape[-1]
+    for stride, size in sorted(zip(s[:-1], shape[:-1])):
         if size > 1:
             if stride < span:
                 raise ValueError(f"elements of {what} overlap")
             span += stride * (size - 1)
+    return (t.data_ptr(), *s[:-1])
 
 
 def _dense(t, shape, dtype, index, what):
     if t is None:
         return 0
-    _fits(t, shape, dtype, index, what)
-    if not t.is_contiguous():
-        raise TypeError(f"{what} must be contiguous")
-    return t.data_ptr()
+    try:
+        if t.dtype is dtype and t.get_device() == index and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, shape, dtype, index, what)
 
 
 def _cache(t, tail, dtype, index, what, rows, slots):
@@ -161,7 +178,7 @@ def _scan_bytes(code, N, L, C, S, G, form):
 
 
 def _workspace(bytes_, like):
-    """From torch's allocator, in units of an fp32 element; a size that is not valid is refused by the call itself."""
+    """From torch's allocator, in fp32 elements; sizes that are not valid are refused by the call itself."""
     return like.new_empty((max(bytes_, 16) + 3) // 4, dtype=_FLOAT32)
 
 
@@ -195,22 +212,21 @@ def dconv_causal(x: torch.Tensor, filt: torch.Tensor, bias: torch.Tensor | None 
     x [N,L,C], filt [C,F] (F <= 8), bias [C], all of one type.  state [N,F-1,C]: the rows before token 0 (default: zeros);
     state_out, which may be `state`, receives the last F-1 rows of each sequence.  lengths [N] int32: the tokens of each
     sequence that count; out is 0 behind them."""
-    dtype, code, index = _first(x, 3, "x")
-    N, L, C = x.shape
+    dtype, code, index, shape = _first(x, 3, "x")
+    N, L, C = shape
     F = _taps(filt, C)
     if out is None:
-        out = x.new_empty((N, L, C))
+        out = x.new_empty(shape)
+        o = out.data_ptr(), L * C, C
     else:
-        _fits(out, x.shape, dtype, index, "out")
-        _apart(out, "out")
+        o = _output(out, shape, dtype, index, "out")
     rows = (N, F - 1, C)
-    args = _CAUSAL.pack(
-        code, N, L, C, F, 0, bool(silu), 0,
-        *_rows(x, (N, L, C), dtype, index, "x"), *_rows(out, (N, L, C), dtype, index, "out"), *_NONE, *_NONE,
-        _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
-        _dense(state, rows, dtype, index, "state"), _dense(state_out, rows, dtype, index, "state_out"), 0, 0, 0, 0,
-        _dense(lengths, (N,), _INT32, index, "lengths"), 0, 0, 0)
-    _run(_lib().dconv_causal, index, args)
+    _run(_lib().dconv_causal, index, _CAUSAL_PROMPT.pack(
+        code, N, L, C, F, 0, bool(silu), 0, *_rows(x, shape, dtype, index, "x"), *o,
+        _dense(filt, (C, F), dtype, index, "filt"), 0 if bias is None else _dense(bias, (C,), dtype, index, "bias"),
+        0 if state is None else _dense(state, rows, dtype, index, "state"),
+        0 if state_out is None else _dense(state_out, rows, dtype, index, "state_out"),
+        0 if lengths is None else _dense(lengths, (N,), _INT32, index, "lengths")))
     return out
 
 
@@ -220,27 +236,25 @@ def dconv_causal_grad(dout: torch.Tensor, x: torch.Tensor, filt: torch.Tensor, b
     """Gradients of dconv_causal(x, filt, bias, ...) from dout, the gradient of its output, and dstate_out, that of state_out.
 
     dx may be given (a slice of a wider gradient, say); it is 0 behind `lengths`.  dstate is None without a state."""
-    dtype, code, index = _first(x, 3, "x")
-    N, L, C = x.shape
+    dtype, code, index, shape = _first(x, 3, "x")
+    N, L, C = shape
     F = _taps(filt, C)
     rows = (N, F - 1, C)
     if dx is None:
-        dx = x.new_empty((N, L, C))
+        dx = x.new_empty(shape)
+        d = dx.data_ptr(), L * C, C
     else:
-        _fits(dx, x.shape, dtype, index, "dx")
-        _apart(dx, "dx")
+        d = _output(dx, shape, dtype, index, "dx")
     dfilt, dbias = x.new_empty((C, F), dtype=_FLOAT32), x.new_empty((C,), dtype=_FLOAT32)
     dstate = None if state is None else x.new_empty(rows)
     need = _causal_bytes(code, N, L, C, F)
     ws = _workspace(need, x)
-    _run(_lib().dconv_causal_grad, index, _CAUSAL.pack(
-        code, N, L, C, F, 0, bool(silu), 0,
-        *_rows(x, (N, L, C), dtype, index, "x"), *_NONE, *_rows(dout, (N, L, C), dtype, index, "dout"),
-        *_rows(dx, (N, L, C), dtype, index, "dx"),
+    _run(_lib().dconv_causal_grad, index, _CAUSAL_GRAD.pack(
+        code, N, L, C, F, 0, bool(silu), 0, *_rows(x, shape, dtype, index, "x"), *_rows(dout, shape, dtype, index, "dout"), *d,
         _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
-        _dense(state, rows, dtype, index, "state"), 0, _dense(dstate_out, rows, dtype, index, "dstate_out"),
+        _dense(state, rows, dtype, index, "state"), _dense(dstate_out, rows, dtype, index, "dstate_out"),
         0 if dstate is None else dstate.data_ptr(), dfilt.data_ptr(), dbias.data_ptr(),
-        _dense(lengths, (N,), _INT32, index, "lengths"), 0, ws.data_ptr(), need))
+        _dense(lengths, (N,), _INT32, index, "lengths"), ws.data_ptr(), need))
     return CausalGrad(dx, dfilt, dbias, dstate)
 
 
@@ -250,53 +264,46 @@ def dconv_causal_step(x: torch.Tensor, state: torch.Tensor, filt: torch.Tensor, 
 
     slots [N] int32: the window of each row (default: row n has window n); rows with a slot outside the cache, or
     one that an earlier row has, are padding: out is 0 there and no window changes."""
-    dtype, code, index = _first(x, 2, "x")
-    N, C = x.shape
+    dtype, code, index, shape = _first(x, 2, "x")
+    N, C = shape
     F = _taps(filt, C)
     if out is None:
-        out = x.new_empty((N, C))
+        out = x.new_empty(shape)
         o = out.data_ptr(), C
     else:
-        o = _row(out, x.shape, dtype, index, "out")
-        _apart(out, "out")
+        o = _output(out, shape, dtype, index, "out")
     cache, M = _cache(state, (F - 1, C), dtype, index, "state", N, slots)
     _run(_lib().dconv_causal_step, index, _CAUSAL_STEP.pack(
-        code, N, 1, C, F, M, bool(silu), 0, *_row(x, x.shape, dtype, index, "x"), *o,
-        _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"), cache,
-        _dense(slots, (N,), _INT32, index, "slots")))
+        code, N, 1, C, F, M, bool(silu), 0, *_row(x, shape, dtype, index, "x"), *o,
+        _dense(filt, (C, F), dtype, index, "filt"), 0 if bias is None else _dense(bias, (C,), dtype, index, "bias"), cache,
+        0 if slots is None else _dense(slots, (N,), _INT32, index, "slots")))
     return out
 
 
 def _taps(filt, C):
-    if not isinstance(filt, torch.Tensor) or filt.dim() != 2 or filt.shape[0] != C:
-        raise ValueError(f"filt must have the shape ({C}, F)")
-    return filt.shape[1]
+    try:
+        c, F = filt.shape
+        if c == C:
+            return F
+    except (AttributeError, ValueError):
+        pass
+    raise ValueError(f"filt must have the shape ({C}, F)")
 
 
 def _scan_sizes(u, A, B, dims):
-    dtype, code, index = _first(u, dims, "u")
-    if not isinstance(A, torch.Tensor) or A.dim() != 2 or A.shape[0] != u.shape[-1]:
+    dtype, code, index, shape = _first(u, dims, "u")
+    if not isinstance(A, torch.Tensor) or A.dim() != 2 or A.shape[0] != shape[-1]:
         raise ValueError("A must have the shape (C, S)")
     if not isinstance(B, torch.Tensor) or B.dim() != dims + 1:
         raise ValueError(f"B must have {dims + 1} dims")
-    return dtype, code, index, A.shape[1], B.shape[-2]
-
-
-def _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index):
-    """What all forms read: the token tensors, and the parameters."""
-    ch, S = A.shape
-    tokens = (_rows(u, wide, dtype, index, "u"), _rows(delta, wide, dtype, index, "delta"), _rows(z, wide, dtype, index, "z"))
-    bc = (_rows(B, narrow, dtype, index, "B"), _rows(C, narrow, dtype, index, "C"))
-    params = (_dense(A, (ch, S), torch.float32, index, "A"), _dense(D, (ch,), torch.float32, index, "D"),
-              _dense(delta_bias, (ch,), torch.float32, index, "delta_bias"))
-    return tokens, bc, params
+    return dtype, code, index, shape, A.shape[1], B.shape[-2]
 
 
 def scan_starts(N: int, L: int, C: int, S: int, G: int = 1, device="cuda") -> torch.Tensor:
     """An empty tensor for the `starts` of dconv_scan and dconv_scan_grad on sequences of these sizes."""
     need = _scan_bytes(DTYPE_F32, N, L, C, S, G, "starts")
     if need < 0:
-        _bad_shape()
+        _package._raise(_package.STATUS_BAD_SHAPE)
     return torch.empty(need // 4, dtype=torch.float32, device=device)
 
 
@@ -319,24 +326,25 @@ def dconv_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.T
     D and delta_bias [C], fp32.  state [N,C,S] fp32: h before token 0 (default: zeros); state_out, which may be `state`,
     receives h behind the last token.  lengths [N] int32: the tokens that count; out is 0 behind them.
     starts (of scan_starts): receives what lets dconv_scan_grad go back without running the scan again."""
-    dtype, code, index, S, G = _scan_sizes(u, A, B, 3)
-    N, L, ch = u.shape
-    wide, narrow = (N, L, ch), (N, L, G, S)
-    tokens, bc, params = _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index)
+    dtype, code, index, wide, S, G = _scan_sizes(u, A, B, 3)
+    N, L, ch = wide
+    narrow = (N, L, G, S)
     if out is None:
         out = u.new_empty(wide)
+        o = out.data_ptr(), L * ch, ch
     else:
-        _fits(out, wide, dtype, index, "out")
-        _apart(out, "out")
+        o = _output(out, wide, dtype, index, "out")
     need = _scan_bytes(code, N, L, ch, S, G, "scan")
     ws = _workspace(need, u) if need else None
-    _run(_lib().dconv_scan, index, _SCAN.pack(
-            code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2],
-            *_rows(out, wide, dtype, index, "out"), *bc[0], *bc[1], *(6 * _NONE), *params,
-            _dense(state, (N, ch, S), torch.float32, index, "state"),
-            _dense(state_out, (N, ch, S), torch.float32, index, "state_out"), 0, 0, 0, 0, 0,
-            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"), 0,
-            0 if ws is None else ws.data_ptr(), need))
+    _run(_lib().dconv_scan, index, _SCAN_PROMPT.pack(
+        code, N, L, ch, S, G, 0, bool(softplus), *_rows(u, wide, dtype, index, "u"), *_rows(delta, wide, dtype, index, "delta"),
+        *_rows(z, wide, dtype, index, "z"), *o, *_groups(B, narrow, dtype, index, "B"), *_groups(C, narrow, dtype, index, "C"),
+        _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
+        _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"),
+        0 if state is None else _dense(state, (N, ch, S), _FLOAT32, index, "state"),
+        0 if state_out is None else _dense(state_out, (N, ch, S), _FLOAT32, index, "state_out"),
+        0 if starts is None else _starts(starts, N, L, ch, S, G, index),
+        0 if lengths is None else _dense(lengths, (N,), _INT32, index, "lengths"), 0 if ws is None else ws.data_ptr(), need))
     return out
 
 
@@ -350,35 +358,36 @@ def dconv_scan_grad(dout: torch.Tensor, u: torch.Tensor, delta: torch.Tensor, A:
 
     starts: what dconv_scan left there for the same inputs; without it the states are made again.  du, ddelta and dz may be
     given (slices of a wider gradient, say); gradients are 0 behind `lengths`."""
-    dtype, code, index, S, G = _scan_sizes(u, A, B, 3)
-    N, L, ch = u.shape
-    wide, narrow = (N, L, ch), (N, L, G, S)
-    tokens, bc, params = _scan_in(u, delta, z, B, C, A, D, delta_bias, wide, narrow, dtype, index)
-    for t, what in ((du, "du"), (ddelta, "ddelta"), (dz, "dz")):
+    dtype, code, index, wide, S, G = _scan_sizes(u, A, B, 3)
+    N, L, ch = wide
+    narrow = (N, L, G, S)
+
+    def wide_out(t, what):
         if t is not None:
-            _fits(t, wide, dtype, index, what)
-            _apart(t, what)
-    du = u.new_empty(wide) if du is None else du
-    ddelta = u.new_empty(wide) if ddelta is None else ddelta
-    if z is None:
-        dz = None
-    elif dz is None:
-        dz = u.new_empty(wide)
+            return t, _output(t, wide, dtype, index, what)
+        t = u.new_empty(wide)
+        return t, (t.data_ptr(), L * ch, ch)
+
+    du, du_ = wide_out(du, "du")
+    ddelta, ddelta_ = wide_out(ddelta, "ddelta")
+    dz, dz_ = (None, _NONE3) if z is None else wide_out(dz, "dz")
     dB, dC, dA = u.new_empty(narrow), u.new_empty(narrow), A.new_empty((ch, S))
     dD = None if D is None else A.new_empty((ch,))
     dbias = None if delta_bias is None else A.new_empty((ch,))
     dstate = None if state is None else A.new_empty((N, ch, S))
-    ptr = lambda t: 0 if t is None else t.data_ptr()
     need = _scan_bytes(code, N, L, ch, S, G, "grad" if starts is None else "starts grad")
     ws = _workspace(need, u)
-    _run(_lib().dconv_scan_grad, index, _SCAN.pack(
-            code, N, L, ch, S, G, 0, bool(softplus), *tokens[0], *tokens[1], *tokens[2], *_NONE, *bc[0], *bc[1],
-            *_rows(dout, wide, dtype, index, "dout"), *_rows(du, wide, dtype, index, "du"),
-            *_rows(ddelta, wide, dtype, index, "ddelta"), *_rows(dz, wide, dtype, index, "dz"),
-            *_rows(dB, narrow, dtype, index, "dB"), *_rows(dC, narrow, dtype, index, "dC"), *params,
-            _dense(state, (N, ch, S), torch.float32, index, "state"), 0,
-            _dense(dstate_out, (N, ch, S), torch.float32, index, "dstate_out"), ptr(dstate), ptr(dA), ptr(dD), ptr(dbias),
-            _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"), 0, ws.data_ptr(), need))
+    _run(_lib().dconv_scan_grad, index, _SCAN_GRAD.pack(
+        code, N, L, ch, S, G, 0, bool(softplus), *_rows(u, wide, dtype, index, "u"), *_rows(delta, wide, dtype, index, "delta"),
+        *_rows(z, wide, dtype, index, "z"), *_groups(B, narrow, dtype, index, "B"), *_groups(C, narrow, dtype, index, "C"),
+        *_rows(dout, wide, dtype, index, "dout"), *du_, *ddelta_, *dz_,
+        dB.data_ptr(), L * G * S, G * S, S, dC.data_ptr(), L * G * S, G * S, S,
+        _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
+        _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"), _dense(state, (N, ch, S), _FLOAT32, index, "state"),
+        _dense(dstate_out, (N, ch, S), _FLOAT32, index, "dstate_out"), 0 if dstate is None else dstate.data_ptr(),
+        dA.data_ptr(), 0 if dD is None else dD.data_ptr(), 0 if dbias is None else dbias.data_ptr(),
+        0 if starts is None else _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"),
+        ws.data_ptr(), need))
     return ScanGrad(du, ddelta, dA, dB, dC, dD, dz, dbias, dstate)
 
 
@@ -389,20 +398,20 @@ def dconv_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: to
     """One token of each row: u, delta, z [N,C], B, C [N,G,S]; out [N,C], and `state` [M,C,S] (fp32) is updated.
 
     slots as for dconv_causal_step."""
-    dtype, code, index, S, G = _scan_sizes(u, A, B, 2)
-    N, ch = u.shape
-    wide, narrow = (N, ch), (N, G, S)
+    dtype, code, index, wide, S, G = _scan_sizes(u, A, B, 2)
+    N, ch = wide
+    narrow = (N, G, S)
     if out is None:
         out = u.new_empty(wide)
         o = out.data_ptr(), ch
     else:
-        o = _row(out, wide, dtype, index, "out")
-        _apart(out, "out")
-    b, c = _rows(B, narrow, dtype, index, "B"), _rows(C, narrow, dtype, index, "C")      # the second stride is the groups'
+        o = _output(out, wide, dtype, index, "out")
     cache, M = _cache(state, (ch, S), _FLOAT32, index, "state", N, slots)
     _run(_lib().dconv_scan_step, index, _SCAN_STEP.pack(
         code, N, 1, ch, S, G, M, bool(softplus), *_row(u, wide, dtype, index, "u"), *_row(delta, wide, dtype, index, "delta"),
-        *((0, 0) if z is None else _row(z, wide, dtype, index, "z")), *o, *b[:3], *c[:3],
+        *((0, 0) if z is None else _row(z, wide, dtype, index, "z")), *o,
+        *_rows(B, narrow, dtype, index, "B"), *_rows(C, narrow, dtype, index, "C"),          # (sequence and group)
         _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
-        _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"), cache, _dense(slots, (N,), _INT32, index, "slots")))
+        _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"), cache,
+        0 if slots is None else _dense(slots, (N,), _INT32, index, "slots")))
     return out

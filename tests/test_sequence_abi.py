@@ -202,12 +202,29 @@ def test_python_functions_refuse_what_does_not_fit():
             pytest.fail(f"call {k} was taken")
 
 
-def test_step_structs_lay_their_fields_where_the_full_ones_have_them():
-    v = list(range(1, 17))
-    full = {"dtype": 1, "N": 2, "L": 3, "C": 4, "F": 5, "M": 6, "silu": 7, "reserved": 8, "x.p": 9, "x.sn": 10, "out.p": 11, "out.sn": 12,
-            "filt": 13, "bias": 14, "state_out": 15, "slots": 16}
-    assert q._CAUSAL_STEP.pack(*v) == _pack(CAUSAL, q._CAUSAL, full)
-    names = ["dtype", "N", "L", "C", "S", "G", "M", "softplus", "u.p", "u.sn", "delta.p", "delta.sn", "z.p", "z.sn", "out.p", "out.sn",
-             "B.p", "B.sn", "B.sg", "Cm.p", "Cm.sn", "Cm.sg", "A", "D", "delta_bias", "state_out", "slots"]
-    v = list(range(1, len(names) + 1))
-    assert q._SCAN_STEP.pack(*v) == _pack(SCAN, q._SCAN, dict(zip(names, v)))
+def test_the_structs_of_each_form_lay_their_fields_where_the_full_ones_have_them():
+    sizes = ["dtype", "N", "L", "C", "F", "M", "silu", "reserved"]
+    rows = lambda *names, fields=("p", "sn", "sl"): [f"{n}.{f}" for n in names for f in fields]
+    forms = [
+        (q._CAUSAL_PROMPT, rows("x", "out") + ["filt", "bias", "state", "state_out", "lengths"]),
+        (q._CAUSAL_GRAD, rows("x", "dout", "dx") + ["filt", "bias", "state", "dstate_out", "dstate", "dfilt", "dbias", "lengths",
+                                                    "workspace", "workspace_bytes"]),
+        (q._CAUSAL_STEP, rows("x", "out", fields=("p", "sn")) + ["filt", "bias", "state_out", "slots"])]
+    for form, names in forms:
+        names = sizes + names
+        v = list(range(1, len(names) + 1))
+        assert form.pack(*v) == _pack(CAUSAL, q._CAUSAL, dict(zip(names, v)))
+    sizes = ["dtype", "N", "L", "C", "S", "G", "M", "softplus"]
+    group = ("p", "sn", "sl", "sg")
+    forms = [
+        (q._SCAN_PROMPT, rows("u", "delta", "z", "out") + rows("B", "Cm", fields=group) +
+         ["A", "D", "delta_bias", "state", "state_out", "starts", "lengths", "workspace", "workspace_bytes"]),
+        (q._SCAN_GRAD, rows("u", "delta", "z") + rows("B", "Cm", fields=group) + rows("dout", "du", "ddelta", "dz") +
+         rows("dB", "dC", fields=group) + ["A", "D", "delta_bias", "state", "dstate_out", "dstate", "dA", "dD", "ddelta_bias",
+                                           "starts", "lengths", "workspace", "workspace_bytes"]),
+        (q._SCAN_STEP, rows("u", "delta", "z", "out", fields=("p", "sn")) + rows("B", "Cm", fields=("p", "sn", "sg")) +
+         ["A", "D", "delta_bias", "state_out", "slots"])]
+    for form, names in forms:
+        names = sizes + names
+        v = list(range(1, len(names) + 1))
+        assert form.pack(*v) == _pack(SCAN, q._SCAN, dict(zip(names, v)))
