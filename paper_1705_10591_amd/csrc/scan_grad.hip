@@ -352,7 +352,8 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
     Run<T, E> un{}, dln{}, gon{}, zn{};
     float hn[R] = {}, cumn = 0.f;
     auto fetch = [&](int tile, int at) {
-        load_states(p.starts + lane_states<W, R>(p, a, (int64_t)a.n * p.tiles + tile, wave, lane), hn);
+        if (p.starts) load_states(p.starts + lane_states<W, R>(p, a, (int64_t)a.n * p.tiles + tile, wave, lane), hn);
+        else if (p.state) load_states(p.state + own, s0, p.S, ok, hn);       // (the only tile)
         if (later) cumn = p.cum[(((int64_t)a.n * p.tiles + tile) * p.blocks + a.block) * kWave + lane];
         if (at < a.len && nv > 0) {
             un = pu.load(nv);
@@ -680,7 +681,7 @@ GradSpace space_of(const dconv_scan_args& a, const ScanPlan& pl)
     s.A_parts = take(states);
     s.D_parts = take(rows);
     s.bias_parts = take(rows);
-    s.starts = take(a.starts ? 0 : scan_starts_floats(a));
+    s.starts = take(a.starts || pl.tiles == 1 ? 0 : scan_starts_floats(a));
     s.all = at;
     return s;
 }
@@ -715,7 +716,7 @@ int dconv_scan_grad(const dconv_scan_args* a, void* stream)
     p.part_bc = ws + s.bc_parts; p.part_A = ws + s.A_parts; p.part_D = ws + s.D_parts; p.part_bias = ws + s.bias_parts;
     rc = launch_scan_bc(*a, pl, ws, st);
     if (rc != DCONV_OK) return rc;
-    if (!a->starts) {
+    if (!a->starts && pl.tiles > 1) {                    // (a single tile begins at the call's state)
         p.starts = ws + s.starts;
         if (pl.chunks > 1) {
             p.ends = ws + s.ends;
