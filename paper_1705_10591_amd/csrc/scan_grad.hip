@@ -39,9 +39,13 @@ __device__ __forceinline__ float fold16(float a, float b)
     return value(r[0]) + value(r[1]);
 }
 
-// lanes with `upper` clear: a over this lane and its partner by CTRL, whose `upper` is the other one; set: b
-template <int CTRL> __device__ __forceinline__ float fold(float a, float b, bool upper)
+// lanes with bit BIT clear: a over this lane and its partner by CTRL, whose bit is the other one; set: b.  The mask of those
+// lanes is a constant: one that is compared for would take a pair of scalar registers.
+template <int CTRL, int BIT> __device__ __forceinline__ float fold(float a, float b)
 {
+    constexpr uint64_t kUpper = BIT == 8 ? 0xff00ff00ff00ff00ull : BIT == 4 ? 0xf0f0f0f0f0f0f0f0ull : BIT == 2 ? 0xccccccccccccccccull
+                                                                                                              : 0xaaaaaaaaaaaaaaaaull;
+    const bool upper = __builtin_amdgcn_inverse_ballot_w64(kUpper);
     const float keep = upper ? b : a, give = upper ? a : b;
     return keep + value(__builtin_amdgcn_update_dpp(0, bits(give), CTRL, 0xf, 0xf, true));
 }
@@ -475,21 +479,21 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
                 qs[j] = q;
                 ys[j] = ea;
                 // lane bit 5: B or C; bits 4 and 3 the state, the rest the token, as far as there are states
-                if constexpr (R == 4) packed[k & 7] = fold<kAcross8>(fold16(pair[0], pair[2]), fold16(pair[1], pair[3]), lane & 8);
+                if constexpr (R == 4) packed[k & 7] = fold<kAcross8, 8>(fold16(pair[0], pair[2]), fold16(pair[1], pair[3]));
                 else packed[k] = fold16(pair[0], pair[R - 1]);
                 if (k % kGather == 0) {
                     float f[4], e[2], g[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         if constexpr (R == 4) g[i] = packed[i];
-                        else g[i] = fold<kAcross8>(packed[i], packed[i + 8], lane & 8);
+                        else g[i] = fold<kAcross8, 8>(packed[i], packed[i + 8]);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) f[i] = fold<kAcross4>(g[i], g[i + 4], lane & 4);
+                    for (int i = 0; i < 4; ++i) f[i] = fold<kAcross4, 4>(g[i], g[i + 4]);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) e[i] = fold<kAcross2>(f[i], f[i + 2], lane & 2);
+                    for (int i = 0; i < 2; ++i) e[i] = fold<kAcross2, 2>(f[i], f[i + 2]);
                     const int64_t at = (((int64_t)a.block * p.N + a.n) * p.tiles + tile) * (kT / kGather) + k / kGather;
-                    p.part_bc[(at * W + wave) * kWave + lane] = fold<kAcross1>(e[0], e[1], lane & 1);
+                    p.part_bc[(at * W + wave) * kWave + lane] = fold<kAcross1, 1>(e[0], e[1]);
                 }
             }
             in_order();
