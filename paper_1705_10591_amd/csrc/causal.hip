@@ -6,7 +6,7 @@
 // step) does that along the tokens: a thread has a run of V channels (16 bytes) and walks a strip of tokens with the
 // last F-1 rows in registers, kAhead rows in flight; lanes next to each other have runs next to each other.  Only the
 // F-1 rows before a strip are read twice.  Measured: 8 x 4096 x 4096 bf16 with 4 taps 116 us, 4.64 TB/s of the 4.94 that a
-// large copy reaches; the gradient of half as many tokens 96 + 5 us; one row of 2048 channels 2.4 us, 200 rows of 5120 5.6.
+// large copy reaches; the gradient of half as many tokens 97 us; one row of 2048 channels 2.4 us, 200 rows of 5120 5.6.
 #include "tokens.h"
 
 namespace dconv {
@@ -341,19 +341,24 @@ bool sizes_ok(const dconv_causal_args& a)
            (double)a.N * a.L * a.C < kMaxElements;
 }
 
-// Elements of a run: 16 bytes; four in gradients, whose windows and sums of eight would leave two waves a SIMD.
-int run_of(const dconv_causal_args& a, bool grad) { return grad ? 4 : 16 / token_bytes(a.dtype); }
+// Elements of a run: 16 bytes.  In gradients two, as windows, sums and two inputs of more leave too few waves to hide a load
+// behind; four of an odd number of channels, whose rows begin anywhere, so that a load costs by lanes and not by bytes.
+// Measured, us with four and two: 4 x 2048 x 2048 bf16 4 taps 32 and 29, the same in fp32 51 and 42, 8 x 2048 x 4096
+// bf16 102 and 99; 4 x 2048 x 4097 bf16 73 and 83, the same in fp32 121 and 150.
+int run_of(const dconv_causal_args& a, bool grad) { return !grad ? 16 / token_bytes(a.dtype) : a.C % 2 ? 4 : 2; }
 
-// Runs and strips of a workgroup (at most 256 threads, `most` runs) and the length of a strip: long ones read fewer
-// rows twice, short ones fill the chip.
+// The length of a strip: long ones read fewer rows twice, short ones fill the chip.  Runs and strips of a workgroup (at most
+// 256 threads, `most` runs): a short call's gradient has 32 runs by 8 strips, so that more of its sums are joined in
+// LDS; measured, us with 64 and 32: 512 x 4096 bf16 11.8 and 10.5, 256 x 256 fp32 10.2 and 9.5, 8 x 2048 x 4096 bf16 99 and 105.
 void lay_out(const dconv_causal_args& a, bool grad, CausalParams* p)
 {
-    const int V = run_of(a, grad), runs = (a.C - 1) / V + 1, most = grad ? 64 : kThreads;
+    const int V = run_of(a, grad), runs = (a.C - 1) / V + 1;
+    p->strip = grad ? 128 : 32;
+    while (p->strip > kAhead && (double)a.N * runs * ((a.L + p->strip - 1) / p->strip) < 262144.0) p->strip /= 2;
+    const int most = !grad ? kThreads : p->strip >= 64 ? 64 : 32;
     p->vgroups = (runs + most - 1) / most;
     p->vb = (runs + p->vgroups - 1) / p->vgroups;
     p->sb = kThreads / p->vb;
-    p->strip = grad ? 64 : 32;
-    while (p->strip > kAhead && (double)a.N * runs * ((a.L + p->strip - 1) / p->strip) < 262144.0) p->strip /= 2;
     const int64_t strips = ((int64_t)a.L + p->strip - 1) / p->strip;
     if (strips < p->sb) p->sb = (int)strips;
     p->sgroups = (int)((strips + p->sb - 1) / p->sb);
@@ -394,13 +399,16 @@ enum class Form { kPrompt, kGrad, kStep };
 
 template <typename T, int F> int launch(Form form, const CausalParams& p, hipStream_t st)
 {
-    constexpr int V = 16 / sizeof(T), VG = 4;
+    constexpr int V = 16 / sizeof(T);
     if (p.total > kMaxThreads / kThreads) return DCONV_BAD_SHAPE;
     const dim3 grid((unsigned)p.total);
     begin_launch();
     switch (form) {
     case Form::kPrompt: hipLaunchKernelGGL((causal_kernel<T, F, V>), grid, dim3(kThreads), 0, st, p); break;
-    case Form::kGrad: hipLaunchKernelGGL((causal_grad_kernel<T, F, VG>), grid, dim3(kThreads), 0, st, p); break;
+    case Form::kGrad:
+        if (p.C % 2) hipLaunchKernelGGL((causal_grad_kernel<T, F, 4>), grid, dim3(kThreads), 0, st, p);
+        else hipLaunchKernelGGL((causal_grad_kernel<T, F, 2>), grid, dim3(kThreads), 0, st, p);
+        break;
     case Form::kStep: hipLaunchKernelGGL((causal_step_kernel<T, F, V>), grid, dim3(kThreads), 0, st, p); break;
     }
     return launch_status();
