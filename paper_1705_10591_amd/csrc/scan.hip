@@ -271,7 +271,7 @@ bool scan_sizes_ok(const dconv_scan_args& a)
         return false;
     // (sizes in floating point, so that no product overflows)
     if ((double)a.N * a.L * a.C * kMaxStates >= kMaxElements) return false;
-    const ScanPlan pl = scan_plan(a, false);             // (a gradient has no more chunks)
+    const ScanPlan pl = scan_plan(a, false);             // (where a gradient has more chunks there are few blocks)
     // (threads of the largest grids: the scans', bc_kernel's, the sums')
     const double bc = (double)a.N * a.G * pl.tiles * pl.waves;
     const double most = (double)kMaxThreads - kThreads;

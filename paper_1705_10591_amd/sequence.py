@@ -68,7 +68,7 @@ def _run(fn, index, args):
         _package._raise(rc)
 
 
-# One token of one row takes the GPU 2.4 us and the host three times as long, most of it in the checks below: a tensor that
+# One token of one row takes the GPU 2.4 us and the host two to three times as long, most of it in the checks below: a tensor that
 # fits is looked at in one expression, and what does not fit is looked into afterwards.  (Sizes of zero are the library's to refuse.)
 
 def _like(t):
