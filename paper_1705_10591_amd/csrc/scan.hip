@@ -205,6 +205,7 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
 #pragma unroll
             for (int k = 0; k < kStep; ++k) ysum[wave][kT - kStep + k][lane] = ys[k];
         }
+        fetched();
         meet();
         if (OUT) finish(tile, t);
     }

@@ -138,6 +138,15 @@ __device__ __forceinline__ void arrived()
     in_order();
 }
 
+// All loads from memory so far are done, and stores (s_waitcnt vmcnt(0)).  The next tile's values are waited for where they have been
+// under way for most of a tile and before this tile's results are stored: at their first use the wait would be for those stores too.
+__device__ __forceinline__ void fetched()
+{
+    in_order();
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    in_order();
+}
+
 // A thread's share of the tiles of a token tensor: one token a tile, E channels.  It walks by whole tiles, so that a tile
 // costs one 64-bit addition.
 template <typename T, int E> struct Share {
