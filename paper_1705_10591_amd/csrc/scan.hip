@@ -290,15 +290,17 @@ ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
     pl.blocks = a.G * pl.gblocks;
     pl.tiles = (a.L + kT - 1) / kT;
     // Chunks cost another launch that does most of the work again, so there are none where the channels alone give the
-    // chip one and a half waves a SIMD (gradients, whose registers let two be there at a time: two), nor for a few tiles.
-    // Otherwise as many as give it eight (gradients: four, and four chunks at least) in chunks of four tiles or more, or
-    // half of that in chunks of two.  Measured with 16 states, us for 1 chunk and for the rule's (sequences x tokens x channels):
+    // chip one and a half waves a SIMD (two in gradients, whose registers let no more be there at a time, and with up to four states,
+    // where most of the work is the channels'), nor for a few tiles.  Otherwise as many as give it eight (six with up to four
+    // states: all that are there at a time; gradients four, and four chunks at least) in chunks of four tiles or more, or half
+    // of that in chunks of two.  Measured with 16 states, us for 1 chunk and for the rule's (sequences x tokens x channels):
     //   scan      1 x 256 x 2048   32, 25   1 x 4096 x 4096   447, 137   3 x 2048 x 4096  227, 177   8 x 2048 x 4096   324, (400)
+    //   4 states  6 x 512 x 4096    59, 51   6 x 2048 x 4096   228, 172   7 x 1024 x 4096  115, 109
     //   gradient  1 x 256 x 2048  104, 50   1 x 4096 x 4096  1500, 350   4 x 2048 x 4096  819, 648   8 x 2048 x 4096  1193, (1205)
     const double alone = (double)a.N * pl.blocks * pl.waves;
     pl.chunks = 1;
-    if (alone < (grad ? 2048 : 1536) && pl.tiles >= (grad ? 6 : 10)) {
-        int most = (int)((grad ? 4096 : 8192) / alone);
+    if (alone < (grad || a.S <= 4 ? 2048 : 1536) && pl.tiles >= (grad ? 6 : 10)) {
+        int most = (int)((grad ? 4096 : a.S <= 4 ? 6144 : 8192) / alone);
         if (grad && most < 4) most = 4;
         const int longer = most < pl.tiles / 4 ? most : pl.tiles / 4, shorter = most / 2 < pl.tiles / 2 ? most / 2 : pl.tiles / 2;
         pl.chunks = longer > shorter ? longer : shorter;
