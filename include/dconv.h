@@ -465,8 +465,8 @@ int dconv_causal(const dconv_causal_args *a, void *stream);
 int dconv_causal_grad(const dconv_causal_args *a, void *stream);
 int dconv_causal_step(const dconv_causal_args *a, void *stream);
 /* Bytes that dconv_causal_grad needs for these sizes (only sizes and dtype are
- * looked at), -1 where they are not valid; host arithmetic.  The other two forms
- * need none. */
+ * looked at), -1 where they are not valid or dfilt and dbias do not fit a launch;
+ * host arithmetic.  The other two forms need none. */
 long long dconv_causal_workspace(const dconv_causal_args *a);
 
 /*

@@ -439,6 +439,10 @@ int launch_typed(Form form, const dconv_causal_args& a, const CausalParams& p, h
 
 int64_t part_rows(const CausalParams& p) { return p.total / p.vgroups; }
 
+// Of causal_sum_kernel, which has more workgroups than causal_grad_kernel where there are few tokens.
+int64_t sum_blocks(const dconv_causal_args& a) { return ((int64_t)(a.F + 1) * a.C + kWave - 1) / kWave; }
+bool sums_fit(const dconv_causal_args& a) { return sum_blocks(a) <= kMaxThreads / kThreads; }
+
 }  // namespace
 
 }  // namespace dconv
@@ -458,7 +462,7 @@ int dconv_causal(const dconv_causal_args* a, void* stream)
 
 long long dconv_causal_workspace(const dconv_causal_args* a)
 {
-    if (!a || !token_bytes(a->dtype) || !sizes_ok(*a)) return -1;
+    if (!a || !token_bytes(a->dtype) || !sizes_ok(*a) || !sums_fit(*a)) return -1;
     CausalParams p{};
     lay_out(*a, true, &p);
     return part_rows(p) * (a->F + 1) * a->C * 4;
@@ -472,6 +476,7 @@ int dconv_causal_grad(const dconv_causal_args* a, void* stream)
     lay_out(*a, true, &p);
     const bool sums = a->dfilt || a->dbias;
     if (sums) {
+        if (!sums_fit(*a)) return DCONV_BAD_SHAPE;
         if (!a->workspace) return DCONV_NULL_POINTER;
         if (!aligned_to(a->workspace, 16)) return DCONV_BAD_SHAPE;
         if (a->workspace_bytes < dconv_causal_workspace(a)) return DCONV_SCRATCH_EXCEEDED;
@@ -479,10 +484,9 @@ int dconv_causal_grad(const dconv_causal_args* a, void* stream)
     }
     rc = launch_typed(Form::kGrad, *a, p, (hipStream_t)stream);
     if (rc != DCONV_OK || !sums) return rc;
-    const int64_t cols = (int64_t)(a->F + 1) * a->C;
     begin_launch();
-    hipLaunchKernelGGL(causal_sum_kernel, dim3((unsigned)((cols + kWave - 1) / kWave)), dim3(kThreads), 0, (hipStream_t)stream,
-                       p.part, part_rows(p), a->C, a->F, a->dfilt, a->dbias);
+    hipLaunchKernelGGL(causal_sum_kernel, dim3((unsigned)sum_blocks(*a)), dim3(kThreads), 0, (hipStream_t)stream, p.part,
+                       part_rows(p), a->C, a->F, a->dfilt, a->dbias);
     return launch_status();
 }
 
