@@ -227,12 +227,20 @@ __device__ __forceinline__ void causal_grad_strip(const CausalParams& p, Place a
             // the row that has all of its terms now; before token 0 it is one of the state
             const int r = t - (F - 1);
             if (r < end && (r >= a.t0 || (a.t0 == 0 && p.dstate))) {
-                float v[V];
+                float v[V] = {};
+                if (r >= 0 && t < len) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    v[i] = 0.f;
+                    for (int j = 0; j < F; ++j)
 #pragma unroll
-                    for (int j = 0; j < F; ++j) v[i] = __builtin_fmaf(w[j][i], ds[F - 1 - j][i], v[i]);
+                        for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(w[j][i], ds[F - 1 - j][i], v[i]);
+                } else {
+                    // beside the sequence there are no terms: 0 times a filter that is not finite would be NaN
+#pragma unroll
+                    for (int j = 0; j < F; ++j)
+                        if (t >= j && t - j < len) {
+#pragma unroll
+                            for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(w[j][i], ds[F - 1 - j][i], v[i]);
+                        }
                 }
                 const int i = r - len + F - 1;               // of state_out, if it went there
                 if (p.dstate_out && i >= 0 && i < F - 1) {
