@@ -47,7 +47,7 @@ __device__ __forceinline__ void scan_block(const ScanParams& p, const ScanPlace&
     const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
 
     float A[R], h[R] = {}, dtotal = 0.f;
-    load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
+    load_decays(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
 #pragma unroll
     for (int r = 0; r < R; ++r) A[r] *= kLog2e;
     const int64_t own = ((int64_t)a.n * p.C + c) * p.S;

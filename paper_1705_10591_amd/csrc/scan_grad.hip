@@ -66,7 +66,7 @@ __device__ __forceinline__ void back_block(const ScanParams& p, const ScanPlace&
     const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
     float A[R], carry[R] = {}, dtotal = 0.f, dbias[E] = {};
     const bool ok = WHOLE || lane < a.nc;
-    load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
+    load_decays(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
 #pragma unroll
     for (int r = 0; r < R; ++r) A[r] *= kLog2e;
     if (a.chunk == p.chunks - 1 && p.dstate_out)
@@ -174,7 +174,7 @@ __device__ __forceinline__ void sweep_block(const ScanParams& p, const ScanPlace
     const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
     const bool ok = WHOLE || lane < a.nc, gate = p.z.p != nullptr;
     float A[R], h[R] = {}, q[R] = {}, decay[R], dtotal = 0.f, dbias[E] = {};
-    load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
+    load_decays(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         A[r] *= kLog2e;
@@ -310,7 +310,7 @@ __device__ __forceinline__ void grad_block(const ScanParams& p, const ScanPlace&
     const int tt = tid / (kWave / E), tc = (tid & (kWave / E - 1)) * E, nv = WHOLE ? E : a.nc - tc, ec = a.c0 + tc;
 
     float A[R], carry[R] = {}, dA[R] = {};
-    load_states(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
+    load_decays(p.A + (int64_t)c * p.S, s0, p.S, ok, A);
     const int64_t own = ((int64_t)a.n * p.C + c) * p.S, row = (int64_t)a.n * p.chunks;
     if (a.chunk == p.chunks - 1) {
         if (p.dstate_out) load_states(p.dstate_out + own, s0, p.S, ok, carry);

@@ -168,12 +168,24 @@ __device__ __forceinline__ int64_t lane_states(const ScanParams& p, const ScanPl
     return (((row * p.blocks + a.block) * W + wave) * kWave + lane) * R;
 }
 
+// A decay constant whose product with log2 e is finite: exp(0 A) is 1 at tokens that do not count and over chunks that hold none,
+// and 0 times an infinity would be NaN.  Steps of more than 5e-37 decay to 0 all the same.  (NaN stays NaN.)
+__device__ __forceinline__ float finite_decay(float a) { return a < -2e38f ? -2e38f : a; }
+
 // The states from s0 on of a channel in a user's [C][S], of which those beyond S are 0.
 template <int R> __device__ __forceinline__ void load_states(const float* p, int s0, int S, bool ok, float (&v)[R])
 {
 #pragma unroll
     for (int r = 0; r < R; ++r) v[r] = 0.f;
     if (ok) load_some<R>(p + s0, S - s0, v);
+}
+
+// ... of the decay constants
+template <int R> __device__ __forceinline__ void load_decays(const float* p, int s0, int S, bool ok, float (&v)[R])
+{
+    load_states(p, s0, S, ok, v);
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = finite_decay(v[r]);
 }
 
 // ... in the library's own arrays

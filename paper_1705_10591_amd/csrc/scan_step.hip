@@ -50,7 +50,7 @@ scan_step_kernel(StepParams p)
     float y = 0.f;
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
-        h[r] = __builtin_fmaf(exp2_(d * (A[r] * kLog2e)), h[r], du * b[r]);
+        h[r] = __builtin_fmaf(exp2_(d * (finite_decay(A[r]) * kLog2e)), h[r], du * b[r]);
         y = __builtin_fmaf(cm[r], h[r], y);
     }
     store_some<kR>(st, p.S - s0, h);
