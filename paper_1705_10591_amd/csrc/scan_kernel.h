@@ -40,7 +40,16 @@ typedef const __attribute__((address_space(4))) f8* bc_ptr;        // constant m
 // B of kStep tokens, and C where it is needed (WITH_C): pairs of tokens, four states each.
 template <bool WITH_C> struct BC {
     f8 vb[kStep / 2], vc[WITH_C ? kStep / 2 : 1];
-    template <typename P> __device__ __forceinline__ void load(P p)              // bc_ptr, or const f8* in LDS
+    // (not one template: a template argument loses the alignment of f8, 16 bytes in the caller's workspace and in LDS)
+    __device__ __forceinline__ void load(bc_ptr p)
+    {
+#pragma unroll
+        for (int i = 0; i < kStep / 2; ++i) {
+            vb[i] = p[2 * i];
+            if (WITH_C) vc[i] = p[2 * i + 1];
+        }
+    }
+    __device__ __forceinline__ void load(const f8* p)
     {
 #pragma unroll
         for (int i = 0; i < kStep / 2; ++i) {

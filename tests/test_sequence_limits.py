@@ -20,3 +20,24 @@ def test_filter_gradients_of_as_many_channels_as_a_launch_holds():
     C = ((1 << 32) - 256) // 4 // 5 // 64 * 64                      # of 4 taps
     need = dconv.load_library().dconv_causal_workspace(_pack(CAUSAL, q._CAUSAL, {"dtype": 1, "N": 1, "L": 1, "C": C, "F": 4}))
     assert need == 5 * C * 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("L,C,S", [(130, 70, 16), (400, 64, 4), (300, 24, 20)])
+def test_workspaces_and_starts_aligned_to_16_bytes_and_no_more(L, C, S, monkeypatch):
+    import torch
+    from test_scan_gpu import _inputs
+    x, st, dout, dlast = _inputs(L, torch.float32, 2, L, C, S, 1)
+    starts = dconv.scan_starts(2, L, C, S)
+    off = torch.empty(starts.numel() + 4, device="cuda")[4:]
+
+    def calls(s):
+        y = dconv.dconv_scan(**x, state=st, starts=s)
+        return [y] + [t for k in (s, None) for t in dconv.dconv_scan_grad(dout, **x, state=st, dstate_out=dlast, starts=k)]
+
+    want = calls(starts)
+    monkeypatch.setattr(q, "_workspace", lambda n, like: like.new_empty((max(n, 16) + 3) // 4 + 4, dtype=torch.float32)[4:])
+    got = calls(off)
+    assert off.data_ptr() % 32 == 16
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
