@@ -41,3 +41,28 @@ def test_gradients_of_filter_and_bias(dtype, N, L, C, F, tokens, parts):
     # rounded on the way to LDS, to memory and to the result
     assert _off(got.dfilt, want[:, :F]) < _allowed(tokens, parts, 3)
     assert _off(got.dbias, want[:, F]) < _allowed(tokens, parts, 3)
+
+
+def _allowed_of(terms, tiles):
+    """Of the norm of the sums of `terms` [N, L, C] over tokens, as the scan's gradients add them up: a thread has every 16th token of a
+    chunk, from the last to the first.  Terms of a gradient differ in size from token to token and are not independent, so that the
+    partial sums are taken as they are instead of sqrt(k) terms: each is rounded to 0.41 * 2^-24 of itself, in the mean, and so is what
+    goes to LDS, to memory and into the result."""
+    N, L, C = terms.shape
+    partial = terms.reshape(N, L // (16 * tiles), tiles, 16, C).flip(2).cumsum(2)
+    chunk = partial[:, :, -1].sum(2)
+    want = chunk.sum((0, 1))
+    squares = sum(t.square().sum() for t in (partial, partial[:, :, -1], chunk, want))
+    return 1.2 * 0.41 * 2.0 ** -24 * (squares.sqrt() / want.norm()).item(), want
+
+
+# tiles whose tokens a thread adds up: chunks of 4, of 2 and of one sequence's 64
+@pytest.mark.parametrize("N,L,C,G,tiles", [(4, 2048, 256, 1, 4), (8, 512, 192, 1, 2), (1, 1024, 512, 512, 64)])
+def test_gradients_of_skip_and_step_bias(N, L, C, G, tiles):
+    """Without a gate dD has terms of dout times u; the bias' gradient adds up ddelta, which is there to be compared with."""
+    from test_scan_gpu import _inputs
+    x, st, dout, dlast = _inputs(L + C, torch.float32, N, L, C, 16, G, gate=False)
+    got = dconv.dconv_scan_grad(dout, **x, state=st, dstate_out=dlast)
+    for name, terms in (("dD", dout.double() * x["u"].double()), ("ddelta_bias", got.ddelta.double())):
+        tol, want = _allowed_of(terms, tiles)
+        assert _off(getattr(got, name), want) < tol, name
