@@ -68,6 +68,12 @@ def _run(fn, index, args):
         _package._raise(rc)
 
 
+def _beyond():
+    """A size that the structs' 32 bits do not hold is one that the library refuses."""
+    _lib()
+    _package._raise(_package.STATUS_BAD_SHAPE)
+
+
 # One token of one row takes the GPU 2.4 us and the host two to three times as long, most of it in the checks below: a tensor that
 # fits is looked at in one expression, and what does not fit is looked into afterwards.  (Sizes of zero are the library's to refuse.)
 
@@ -169,14 +175,21 @@ def _cache(t, tail, dtype, index, what, rows, slots):
 
 @lru_cache(maxsize=4096)
 def _causal_bytes(code, N, L, C, F):
-    return _lib().dconv_causal_workspace(_CAUSAL.pack(code, N, L, C, F, 0, 0, 0, *(4 * _NONE), *(12 * (0,))))
+    try:
+        args = _CAUSAL.pack(code, N, L, C, F, 0, 0, 0, *(4 * _NONE), *(12 * (0,)))
+    except struct.error:
+        _beyond()
+    return _lib().dconv_causal_workspace(args)
 
 
 @lru_cache(maxsize=4096)
 def _scan_bytes(code, N, L, C, S, G, form):
     """Of the workspace of a prompt ("scan"), a gradient with and without starts ("grad", "starts grad"), of the starts."""
     tokens = (*(3 * _NONE), 16, 0, 0, 0, *(8 * _NONE))               # (a prompt that has an output)
-    args = _SCAN.pack(code, N, L, C, S, G, 0, 0, *tokens, *(10 * (0,)), 16 if form == "starts grad" else 0, 0, 0, 0, 0)
+    try:
+        args = _SCAN.pack(code, N, L, C, S, G, 0, 0, *tokens, *(10 * (0,)), 16 if form == "starts grad" else 0, 0, 0, 0, 0)
+    except struct.error:
+        _beyond()
     if form == "starts":
         return _lib().dconv_scan_starts(args)
     return _lib().dconv_scan_workspace(args, 0 if form == "scan" else 1)
@@ -226,12 +239,16 @@ def dconv_causal(x: torch.Tensor, filt: torch.Tensor, bias: torch.Tensor | None 
     else:
         o = _output(out, shape, dtype, index, "out")
     rows = (N, F - 1, C)
-    _run(_lib().dconv_causal, index, _CAUSAL_PROMPT.pack(
-        code, N, L, C, F, 0, bool(silu), 0, *_rows(x, shape, dtype, index, "x"), *o,
-        _dense(filt, (C, F), dtype, index, "filt"), 0 if bias is None else _dense(bias, (C,), dtype, index, "bias"),
-        0 if state is None else _dense(state, rows, dtype, index, "state"),
-        0 if state_out is None else _dense(state_out, rows, dtype, index, "state_out"),
-        0 if lengths is None else _dense(lengths, (N,), _INT32, index, "lengths")))
+    try:
+        args = _CAUSAL_PROMPT.pack(
+            code, N, L, C, F, 0, bool(silu), 0, *_rows(x, shape, dtype, index, "x"), *o,
+            _dense(filt, (C, F), dtype, index, "filt"), 0 if bias is None else _dense(bias, (C,), dtype, index, "bias"),
+            0 if state is None else _dense(state, rows, dtype, index, "state"),
+            0 if state_out is None else _dense(state_out, rows, dtype, index, "state_out"),
+            0 if lengths is None else _dense(lengths, (N,), _INT32, index, "lengths"))
+    except struct.error:
+        _beyond()
+    _run(_lib().dconv_causal, index, args)
     return out
 
 
@@ -254,12 +271,16 @@ def dconv_causal_grad(dout: torch.Tensor, x: torch.Tensor, filt: torch.Tensor, b
     dstate = None if state is None else _like(state)
     need = _causal_bytes(code, N, L, C, F)
     ws = _workspace(need, x)
-    _run(_lib().dconv_causal_grad, index, _CAUSAL_GRAD.pack(
-        code, N, L, C, F, 0, bool(silu), 0, *_rows(x, shape, dtype, index, "x"), *_rows(dout, shape, dtype, index, "dout"), *d,
-        _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
-        _dense(state, rows, dtype, index, "state"), _dense(dstate_out, rows, dtype, index, "dstate_out"),
-        0 if dstate is None else dstate.data_ptr(), dfilt.data_ptr(), dbias.data_ptr(),
-        _dense(lengths, (N,), _INT32, index, "lengths"), ws.data_ptr(), need))
+    try:
+        args = _CAUSAL_GRAD.pack(
+            code, N, L, C, F, 0, bool(silu), 0, *_rows(x, shape, dtype, index, "x"), *_rows(dout, shape, dtype, index, "dout"), *d,
+            _dense(filt, (C, F), dtype, index, "filt"), _dense(bias, (C,), dtype, index, "bias"),
+            _dense(state, rows, dtype, index, "state"), _dense(dstate_out, rows, dtype, index, "dstate_out"),
+            0 if dstate is None else dstate.data_ptr(), dfilt.data_ptr(), dbias.data_ptr(),
+            _dense(lengths, (N,), _INT32, index, "lengths"), ws.data_ptr(), need)
+    except struct.error:
+        _beyond()
+    _run(_lib().dconv_causal_grad, index, args)
     return CausalGrad(dx, dfilt, dbias, dstate)
 
 
@@ -278,10 +299,14 @@ def dconv_causal_step(x: torch.Tensor, state: torch.Tensor, filt: torch.Tensor, 
     else:
         o = _output(out, shape, dtype, index, "out")
     cache, M = _cache(state, (F - 1, C), dtype, index, "state", N, slots)
-    _run(_lib().dconv_causal_step, index, _CAUSAL_STEP.pack(
-        code, N, 1, C, F, M, bool(silu), 0, *_row(x, shape, dtype, index, "x"), *o,
-        _dense(filt, (C, F), dtype, index, "filt"), 0 if bias is None else _dense(bias, (C,), dtype, index, "bias"), cache,
-        0 if slots is None else _dense(slots, (N,), _INT32, index, "slots")))
+    try:
+        args = _CAUSAL_STEP.pack(
+            code, N, 1, C, F, M, bool(silu), 0, *_row(x, shape, dtype, index, "x"), *o,
+            _dense(filt, (C, F), dtype, index, "filt"), 0 if bias is None else _dense(bias, (C,), dtype, index, "bias"), cache,
+            0 if slots is None else _dense(slots, (N,), _INT32, index, "slots"))
+    except struct.error:
+        _beyond()
+    _run(_lib().dconv_causal_step, index, args)
     return out
 
 
@@ -341,15 +366,19 @@ def dconv_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.T
         o = _output(out, wide, dtype, index, "out")
     need = _scan_bytes(code, N, L, ch, S, G, "scan")
     ws = _workspace(need, u) if need else None
-    _run(_lib().dconv_scan, index, _SCAN_PROMPT.pack(
-        code, N, L, ch, S, G, 0, bool(softplus), *_rows(u, wide, dtype, index, "u"), *_rows(delta, wide, dtype, index, "delta"),
-        *_rows(z, wide, dtype, index, "z"), *o, *_groups(B, narrow, dtype, index, "B"), *_groups(C, narrow, dtype, index, "C"),
-        _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
-        _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"),
-        0 if state is None else _dense(state, (N, ch, S), _FLOAT32, index, "state"),
-        0 if state_out is None else _dense(state_out, (N, ch, S), _FLOAT32, index, "state_out"),
-        0 if starts is None else _starts(starts, N, L, ch, S, G, index),
-        0 if lengths is None else _dense(lengths, (N,), _INT32, index, "lengths"), 0 if ws is None else ws.data_ptr(), need))
+    try:
+        args = _SCAN_PROMPT.pack(
+            code, N, L, ch, S, G, 0, bool(softplus), *_rows(u, wide, dtype, index, "u"), *_rows(delta, wide, dtype, index, "delta"),
+            *_rows(z, wide, dtype, index, "z"), *o, *_groups(B, narrow, dtype, index, "B"), *_groups(C, narrow, dtype, index, "C"),
+            _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
+            _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"),
+            0 if state is None else _dense(state, (N, ch, S), _FLOAT32, index, "state"),
+            0 if state_out is None else _dense(state_out, (N, ch, S), _FLOAT32, index, "state_out"),
+            0 if starts is None else _starts(starts, N, L, ch, S, G, index),
+            0 if lengths is None else _dense(lengths, (N,), _INT32, index, "lengths"), 0 if ws is None else ws.data_ptr(), need)
+    except struct.error:
+        _beyond()
+    _run(_lib().dconv_scan, index, args)
     return out
 
 
@@ -382,17 +411,21 @@ def dconv_scan_grad(dout: torch.Tensor, u: torch.Tensor, delta: torch.Tensor, A:
     dstate = None if state is None else _like(state)
     need = _scan_bytes(code, N, L, ch, S, G, "grad" if starts is None else "starts grad")
     ws = _workspace(need, u)
-    _run(_lib().dconv_scan_grad, index, _SCAN_GRAD.pack(
-        code, N, L, ch, S, G, 0, bool(softplus), *_rows(u, wide, dtype, index, "u"), *_rows(delta, wide, dtype, index, "delta"),
-        *_rows(z, wide, dtype, index, "z"), *_groups(B, narrow, dtype, index, "B"), *_groups(C, narrow, dtype, index, "C"),
-        *_rows(dout, wide, dtype, index, "dout"), *du_, *ddelta_, *dz_,
-        dB.data_ptr(), L * G * S, G * S, S, dC.data_ptr(), L * G * S, G * S, S,
-        _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
-        _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"), _dense(state, (N, ch, S), _FLOAT32, index, "state"),
-        _dense(dstate_out, (N, ch, S), _FLOAT32, index, "dstate_out"), 0 if dstate is None else dstate.data_ptr(),
-        dA.data_ptr(), 0 if dD is None else dD.data_ptr(), 0 if dbias is None else dbias.data_ptr(),
-        0 if starts is None else _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"),
-        ws.data_ptr(), need))
+    try:
+        args = _SCAN_GRAD.pack(
+            code, N, L, ch, S, G, 0, bool(softplus), *_rows(u, wide, dtype, index, "u"), *_rows(delta, wide, dtype, index, "delta"),
+            *_rows(z, wide, dtype, index, "z"), *_groups(B, narrow, dtype, index, "B"), *_groups(C, narrow, dtype, index, "C"),
+            *_rows(dout, wide, dtype, index, "dout"), *du_, *ddelta_, *dz_,
+            dB.data_ptr(), L * G * S, G * S, S, dC.data_ptr(), L * G * S, G * S, S,
+            _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
+            _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"), _dense(state, (N, ch, S), _FLOAT32, index, "state"),
+            _dense(dstate_out, (N, ch, S), _FLOAT32, index, "dstate_out"), 0 if dstate is None else dstate.data_ptr(),
+            dA.data_ptr(), 0 if dD is None else dD.data_ptr(), 0 if dbias is None else dbias.data_ptr(),
+            0 if starts is None else _starts(starts, N, L, ch, S, G, index), _dense(lengths, (N,), _INT32, index, "lengths"),
+            ws.data_ptr(), need)
+    except struct.error:
+        _beyond()
+    _run(_lib().dconv_scan_grad, index, args)
     return ScanGrad(du, ddelta, dA, dB, dC, dD, dz, dbias, dstate)
 
 
@@ -412,11 +445,15 @@ def dconv_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: to
     else:
         o = _output(out, wide, dtype, index, "out")
     cache, M = _cache(state, (ch, S), _FLOAT32, index, "state", N, slots)
-    _run(_lib().dconv_scan_step, index, _SCAN_STEP.pack(
-        code, N, 1, ch, S, G, M, bool(softplus), *_row(u, wide, dtype, index, "u"), *_row(delta, wide, dtype, index, "delta"),
-        *((0, 0) if z is None else _row(z, wide, dtype, index, "z")), *o,
-        *_rows(B, narrow, dtype, index, "B"), *_rows(C, narrow, dtype, index, "C"),          # (sequence and group)
-        _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
-        _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"), cache,
-        0 if slots is None else _dense(slots, (N,), _INT32, index, "slots")))
+    try:
+        args = _SCAN_STEP.pack(
+            code, N, 1, ch, S, G, M, bool(softplus), *_row(u, wide, dtype, index, "u"), *_row(delta, wide, dtype, index, "delta"),
+            *((0, 0) if z is None else _row(z, wide, dtype, index, "z")), *o,
+            *_rows(B, narrow, dtype, index, "B"), *_rows(C, narrow, dtype, index, "C"),          # (sequence and group)
+            _dense(A, (ch, S), _FLOAT32, index, "A"), _dense(D, (ch,), _FLOAT32, index, "D"),
+            _dense(delta_bias, (ch,), _FLOAT32, index, "delta_bias"), cache,
+            0 if slots is None else _dense(slots, (N,), _INT32, index, "slots"))
+    except struct.error:
+        _beyond()
+    _run(_lib().dconv_scan_step, index, args)
     return out

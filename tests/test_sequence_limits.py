@@ -41,3 +41,23 @@ def test_workspaces_and_starts_aligned_to_16_bytes_and_no_more(L, C, S, monkeypa
     assert off.data_ptr() % 32 == 16
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("sizes", [(1 << 31, 4, 64, 16), (1, 1 << 31, 64, 16), (1, 4, 1 << 31, 16), (1, 4, 64, 1 << 40)])
+def test_starts_of_sizes_beyond_32_bits_are_a_bad_shape(sizes):
+    with pytest.raises(dconv.DconvError) as e:
+        dconv.scan_starts(*sizes)
+    assert e.value.status == SHAPE
+
+
+@pytest.mark.gpu
+def test_more_rows_than_32_bits_are_a_bad_shape():
+    import torch
+    many = lambda *s, t=torch.bfloat16: torch.zeros((1, *s), dtype=t, device="cuda").expand(1 << 31, *s)      # one row of memory
+    w, A = torch.zeros((1, 4), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, 1), device="cuda")
+    x, B = many(1, 1), many(1, 1, 1)
+    for call in (lambda: dconv.dconv_causal(x, w), lambda: dconv.dconv_causal_grad(x, x, w), lambda: dconv.dconv_scan(x, x, A, B, B),
+                 lambda: dconv.dconv_scan_grad(x, x, x, A, B, B)):
+        with pytest.raises(dconv.DconvError) as e:
+            call()
+        assert e.value.status == SHAPE
