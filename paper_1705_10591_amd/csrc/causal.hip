@@ -368,9 +368,10 @@ bool sizes_ok(const dconv_causal_args& a)
 }
 
 // Elements of a run: 16 bytes.  In gradients two, as windows, sums and two inputs of more leave too few waves to hide a load
-// behind; four of an odd number of channels, whose rows begin anywhere, so that a load costs by lanes and not by bytes.
-// Measured, us with four and two: 4 x 2048 x 2048 bf16 4 taps 32 and 29, the same in fp32 51 and 42, 8 x 2048 x 4096
-// bf16 102 and 99; 4 x 2048 x 4097 bf16 73 and 83, the same in fp32 121 and 150.
+// behind, and four of an odd number of channels, whose last run is cut.  Sizes alone choose, as the workspace depends on it; that rows
+// begin at odd elements makes no difference.  Measured, us with two and four, 4 taps:
+//   bf16  4 x 2048 x 2048 32 and 35 (31 and 34 as slices of rows of 4097), x 2049 52 and 46, x 4097 117 and 89, 3 x 1021 x 770 16 and 21
+//   fp32  4 x 2048 x 2048 55 and 61 (58 and 66 as slices of rows of 4097), x 2049 82 and 75, x 4097 188 and 137, 3 x 1021 x 770 17 and 23
 int run_of(const dconv_causal_args& a, bool grad) { return !grad ? 16 / token_bytes(a.dtype) : a.C % 2 ? 4 : 2; }
 
 // The length of a strip: long ones read fewer rows twice, short ones fill the chip.  Runs and strips of a workgroup (at most
@@ -423,7 +424,7 @@ CausalParams params_of(const dconv_causal_args& a)
 
 enum class Form { kPrompt, kGrad, kStep };
 
-template <typename T, int F> int launch(Form form, const CausalParams& p, hipStream_t st)
+template <typename T, int F> int launch(Form form, int run, const CausalParams& p, hipStream_t st)
 {
     constexpr int V = 16 / sizeof(T);
     if (p.total > kMaxThreads / kThreads) return DCONV_BAD_SHAPE;
@@ -432,7 +433,7 @@ template <typename T, int F> int launch(Form form, const CausalParams& p, hipStr
     switch (form) {
     case Form::kPrompt: hipLaunchKernelGGL((causal_kernel<T, F, V>), grid, dim3(kThreads), 0, st, p); break;
     case Form::kGrad:
-        if (p.C % 2) hipLaunchKernelGGL((causal_grad_kernel<T, F, 4>), grid, dim3(kThreads), 0, st, p);
+        if (run == 4) hipLaunchKernelGGL((causal_grad_kernel<T, F, 4>), grid, dim3(kThreads), 0, st, p);
         else hipLaunchKernelGGL((causal_grad_kernel<T, F, 2>), grid, dim3(kThreads), 0, st, p);
         break;
     case Form::kStep: hipLaunchKernelGGL((causal_step_kernel<T, F, V>), grid, dim3(kThreads), 0, st, p); break;
@@ -440,26 +441,27 @@ template <typename T, int F> int launch(Form form, const CausalParams& p, hipStr
     return launch_status();
 }
 
-template <typename T> int launch_taps(Form form, int F, const CausalParams& p, hipStream_t st)
+template <typename T> int launch_taps(Form form, int F, int run, const CausalParams& p, hipStream_t st)
 {
     switch (F) {
-    case 1: return launch<T, 1>(form, p, st);
-    case 2: return launch<T, 2>(form, p, st);
-    case 3: return launch<T, 3>(form, p, st);
-    case 4: return launch<T, 4>(form, p, st);
-    case 5: return launch<T, 5>(form, p, st);
-    case 6: return launch<T, 6>(form, p, st);
-    case 7: return launch<T, 7>(form, p, st);
-    default: return launch<T, 8>(form, p, st);
+    case 1: return launch<T, 1>(form, run, p, st);
+    case 2: return launch<T, 2>(form, run, p, st);
+    case 3: return launch<T, 3>(form, run, p, st);
+    case 4: return launch<T, 4>(form, run, p, st);
+    case 5: return launch<T, 5>(form, run, p, st);
+    case 6: return launch<T, 6>(form, run, p, st);
+    case 7: return launch<T, 7>(form, run, p, st);
+    default: return launch<T, 8>(form, run, p, st);
     }
 }
 
 int launch_typed(Form form, const dconv_causal_args& a, const CausalParams& p, hipStream_t st)
 {
+    const int run = run_of(a, form == Form::kGrad);
     switch (a.dtype) {
-    case DCONV_DTYPE_F16: return launch_taps<_Float16>(form, a.F, p, st);
-    case DCONV_DTYPE_BF16: return launch_taps<__bf16>(form, a.F, p, st);
-    default: return launch_taps<float>(form, a.F, p, st);
+    case DCONV_DTYPE_F16: return launch_taps<_Float16>(form, a.F, run, p, st);
+    case DCONV_DTYPE_BF16: return launch_taps<__bf16>(form, a.F, run, p, st);
+    default: return launch_taps<float>(form, a.F, run, p, st);
     }
 }
 

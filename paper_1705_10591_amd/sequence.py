@@ -344,7 +344,7 @@ def _starts(starts, N, L, C, S, G, index):
     return _dense(starts, (max(need, 0) // 4,), torch.float32, index, "starts")
 
 
-def dconv_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor | None,
+def dconv_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor,
                D: torch.Tensor | None = None, z: torch.Tensor | None = None, delta_bias: torch.Tensor | None = None, *,
                softplus: bool = True, state: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
                out: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
