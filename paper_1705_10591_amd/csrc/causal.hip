@@ -6,7 +6,7 @@
 // step) does that along the tokens: a thread has a run of V channels (16 bytes) and walks a strip of tokens with the
 // last F-1 rows in registers, kAhead rows in flight; lanes next to each other have runs next to each other.  Only the
 // F-1 rows before a strip are read twice.  Measured: 8 x 4096 x 4096 bf16 with 4 taps 116 us, 4.64 TB/s of the 4.94 that a
-// large copy reaches; the gradient of half as many tokens 97 us; one row of 2048 channels 2.4 us, 200 rows of 5120 5.6.
+// large copy reaches; the gradient of half as many tokens 98 us; one row of 2048 channels 2.4 us, 200 rows of 5120 5.6.
 #include "tokens.h"
 
 namespace dconv {

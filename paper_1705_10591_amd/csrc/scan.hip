@@ -292,11 +292,17 @@ ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
     // Chunks cost another launch that does most of the work again, so there are none where the channels alone give the
     // chip one and a half waves a SIMD (two in gradients, whose registers let no more be there at a time, and with up to four states,
     // where most of the work is the channels'), nor for a few tiles.  Otherwise as many as give it eight (six with up to four
-    // states: all that are there at a time; gradients four, and four chunks at least) in chunks of four tiles or more, or half
-    // of that in chunks of two.  Measured with 16 states, us for 1 chunk and for the rule's (sequences x tokens x channels):
-    //   scan      1 x 256 x 2048   32, 25   1 x 4096 x 4096   447, 137   3 x 2048 x 4096  227, 177   8 x 2048 x 4096   324, (400)
-    //   4 states  6 x 512 x 4096    59, 51   6 x 2048 x 4096   228, 172   7 x 1024 x 4096  115, 109
-    //   gradient  1 x 256 x 2048  104, 50   1 x 4096 x 4096  1500, 350   4 x 2048 x 4096  819, 648   8 x 2048 x 4096  1193, (1205)
+    // states, of which six are there at a time in 16 bits and five in fp32; gradients four, and four chunks at least) in chunks of four
+    // tiles or more, or half of that in chunks of two.  Measured in bf16 with 16 states, us for 1 chunk and for the rule's (sequences x
+    // tokens x channels; in brackets what the rule leaves in one):
+    //   scan      1 x 256 x 2048   32, 20   1 x 4096 x 4096   422, 132   3 x 2048 x 4096  216, 171   8 x 2048 x 4096   306, (387)
+    //   4 states  6 x 512 x 4096    61, 50   6 x 2048 x 4096   228, 168, in fp32 267, 258            7 x 1024 x 4096   120, 107
+    //   gradient  1 x 256 x 2048  101, 35   1 x 4096 x 4096  1408, 318   4 x 2048 x 4096  753, 604   8 x 2048 x 4096  1132, (1152)
+    // Few channels make many chunks, and each workgroup joins all those before its own, one memory round trip at a time:
+    //   scan      1 x 16384 x 64   1681, 163 (512 chunks)   1 x 16384 x 256  1684, 108   1 x 131072 x 64   13396, 667 (2048 chunks)
+    //   gradient  1 x 16384 x 64   5587, 203                1 x 16384 x 256  5580, 248   1 x 131072 x 64   44754, 799
+    // No more chunks than the square root of twice the tiles would take 85, 90, 234 and 166, 172, 458 there, but 67 instead of 47 for
+    // the gradient of 1 x 2048 x 128.
     const double alone = (double)a.N * pl.blocks * pl.waves;
     pl.chunks = 1;
     if (alone < (grad || a.S <= 4 ? 2048 : 1536) && pl.tiles >= (grad ? 6 : 10)) {
@@ -312,8 +318,8 @@ ScanPlan scan_plan(const dconv_scan_args& a, bool grad)
 }
 
 // Short calls: up to six tiles where the chip has at most two waves a SIMD.  Measured, us a call without and with
-// (sequences x tokens x channels, 16 states): 1 x 16 x 2048 20, 16.5; 1 x 64 x 2048 20, 17; 8 x 64 x 4096 20.3, 19.2;
-// 32 x 64 x 4096 43, 47; 8 x 256 x 4096 47, 49.5; 8 x 1024 x 4096 163, 176.
+// (sequences x tokens x channels, 16 states, bf16): 1 x 16 x 2048 16.5, 12.0; 1 x 64 x 2048 16.7, 12.0; 8 x 64 x 4096 17.6, 15.5;
+// 32 x 64 x 4096 40.4, 43.3; 8 x 256 x 4096 43.6, 45.2; 8 x 1024 x 4096 152, 167.
 bool scan_short(const dconv_scan_args& a, const ScanPlan& pl)
 {
     return a.out.p && pl.chunks == 1 && pl.tiles <= 6 && (double)a.N * pl.blocks * pl.waves <= 2048;

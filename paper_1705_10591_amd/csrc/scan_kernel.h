@@ -21,9 +21,9 @@
 //    runs each chunk from a state of zero, and each workgroup of the second begins by putting together what the chunks
 //    before it leave, since a chunk changes the state it is given by the factor exp(A sum d) alone.
 //
-// Measured, bf16, 16 states: 16 x 2048 x 4096 in 540 us, 39 clocks for 64 (token, channel, state) of which the five
-// instructions above are 24 (exp2 takes 9, a multiply-add 4.7); 1 x 16384 x 4096 in two passes 215 + 296 us; 4 x 2048 x 4096
-// gradient 172 + 461 + 15 us.
+// Measured, bf16, 16 states: 16 x 2048 x 4096 in 525 us, 38 clocks for 64 (token, channel, state) of which the five
+// instructions above are 25 (20 for the chain of product, exponential, product and multiply-add, 4.7 for another multiply-add;
+// by itself exp2 takes 9); 1 x 16384 x 4096 in two passes 184 + 249 us; 4 x 2048 x 4096 gradient 160 + 423 + 16 us.
 #pragma once
 #include "tokens.h"
 

@@ -3,7 +3,8 @@
 Token tensors are [N, L, C] (B and C of the scan [N, L, G, S]) with the last dimension contiguous and any strides before
 it; a step has no L.  As everywhere in this package, functions check and marshal arguments, enqueue on the current stream
 of the tensors' device and return; outputs that are not passed in, and workspaces, come from torch's allocator, which
-is safe for streams and captured graphs.  Gradients are explicit calls: nothing is recorded for torch.autograd.
+is safe for streams and captured graphs.  Outputs must not share memory with inputs, but for the states that a call says it may
+write over.  Gradients are explicit calls: nothing is recorded for torch.autograd.
 """
 from __future__ import annotations
 
