@@ -489,6 +489,8 @@ long long dconv_causal_workspace(const dconv_causal_args *a);
  * Decays exp(d * A) are meant to be at most 1 (A <= 0, d >= 0).  Larger ones are
  * computed as they are; where their product over a sequence passes the largest
  * fp32 number, results may be infinite or NaN.
+ * An A below -2e38 (-inf among them) is taken as that: no step of a token
+ * leaves anything of the state, and no token does nothing to it.
  */
 typedef struct dconv_scan_args {
     int dtype, N, L, C, S, G, M, softplus;
